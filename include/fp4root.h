@@ -322,6 +322,130 @@ int fp4root_qadamw_update(uint16_t* w, const float* g, float* m, int64_t n, uint
                           uint32_t flags, uint64_t seed, int32_t step, void* ws, size_t ws_bytes,
                           void* stream);
 
+/* ---- gradient norm and clipping ------------------------------------------------- */
+
+/* Element types of the operators that take more than one. */
+enum { FP4ROOT_FLOAT32 = 0, FP4ROOT_BFLOAT16 = 1, FP4ROOT_FLOAT16 = 2 };
+
+/* Norms. */
+enum {
+  FP4ROOT_NORM_L2 = 0,  /* total = sum x^2 (binary64), norm = sqrt(total) */
+  FP4ROOT_NORM_MAX = 1  /* total = max |x|,            norm = total       */
+};
+
+/* One tensor of a gradient list: rows x cols elements of type in_type at `in` (device, at
+ * the element's alignment), row stride ld_in >= cols; a contiguous tensor of any shape may be
+ * given as one row.  rows or cols may be 0 (then the pointers may be NULL).  out, ld_out and
+ * out_type: where fp4root_clip_grads writes; fp4root_grad_norm does not read them. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t rows, cols, ld_in, ld_out;
+  int32_t in_type, out_type;
+} fp4root_tensor;
+
+/* Workspace bytes fp4root_grad_norm needs for this list, or 0 for an invalid one. */
+size_t fp4root_grad_norm_workspace(const fp4root_tensor* tensors, int64_t count);
+
+/* The norm of all elements of `count` tensors (host array, at most 2^20) taken together.
+ *   kind:   FP4ROOT_NORM_*; max_norm: > 0 (+inf: no clipping); eps: >= 0, finite;
+ *   total:  device double, the sum of squares or the largest magnitude: what ranks that hold
+ *           shards of the gradients add (or take the maximum of) before fp4root_clip_coef;
+ *   norms:  device floats, each tensor's own norm (0 for an empty one), or NULL;
+ *   result: device floats: result[0] = the norm, result[1] = the clipping coefficient
+ *           min(1, max_norm / (norm + eps)), formed in binary64 and rounded once.
+ * Squares are exact in binary64 and summed there in an order that depends on each tensor's
+ * size alone, so nothing overflows, a tensor's norm does not change with the tensors beside it
+ * and repeated calls give the same bits.  A NaN makes the norms it enters and the coefficient
+ * NaN; an infinity makes the norms infinite and the coefficient 0 (NaN where max_norm is
+ * infinite too); both are reported by fp4root_device_status(ws). */
+int fp4root_grad_norm(const fp4root_tensor* tensors, int64_t count, int kind, double max_norm, double eps,
+                      double* total, float* norms, float* result, void* ws, size_t ws_bytes, void* stream);
+
+/* result (as above) from a total on the device. */
+int fp4root_clip_coef(const double* total, int kind, double max_norm, double eps, float* result, void* stream);
+
+/* out = round(fl32(in * *coef)) for every tensor of the list, coef a device float (result + 1
+ * above).  out may be in itself, with the same type and stride (tensors that the coefficient 1
+ * leaves as they are, are then not touched); any other overlap of an output with another
+ * tensor of the list, or one tensor written twice, is refused.  A result past the output
+ * type's largest becomes an infinity.  count is at most 2^20. */
+int fp4root_clip_grads(const fp4root_tensor* tensors, int64_t count, const float* coef, void* stream);
+
+/* fp4root_momentum_update, fp4root_qadamw_update and fp4root_root_step with every gradient
+ * element g replaced by fl32(g * *grad_scale), grad_scale a device float: clipping without
+ * another pass over the gradients.  The same bits as after fp4root_clip_grads in place;
+ * NULL: the gradients as they are. */
+int fp4root_momentum_update_scaled(const float* g, float* m, int64_t batch, int64_t rows, int64_t cols,
+                                   uint8_t* codes, uint8_t* scales, float* tensor_scale, float beta,
+                                   uint32_t flags, uint64_t seed, int32_t step, const float* grad_scale,
+                                   void* ws, size_t ws_bytes, void* stream);
+int fp4root_qadamw_update_scaled(uint16_t* w, const float* g, float* m, int64_t n, uint8_t* m_codes,
+                                 uint8_t* m_scales, float* m_tensor_scale, uint8_t* v_codes,
+                                 uint16_t* v_scales, uint16_t* v_means, float lr, float wd, float beta1,
+                                 float beta2, float eps, uint32_t flags, uint64_t seed, int32_t step,
+                                 const float* grad_scale, void* ws, size_t ws_bytes, void* stream);
+int fp4root_root_step_scaled(const fp4root_param* params, int64_t count, const fp4root_root_config* rc,
+                             const fp4root_ns_config* ns, const float* grad_scale, void* ws, size_t ws_bytes,
+                             void* stream);
+
+/* ---- root-mean-square norm before a quantized projection ------------------------ */
+
+/* Scales of an 8-bit output. */
+enum {
+  FP4ROOT_SCALE_FP32 = 0, /* s = fl32(amax / 448)                                             */
+  FP4ROOT_SCALE_E8M0 = 1  /* the smallest power of two with amax <= 448 s, as its biased
+                             exponent (OCP MX E8M0, bias 127): nothing saturates              */
+};
+
+/* One call of fp4root_rmsnorm_quantize (host memory; device pointers at their element's
+ * alignment; row strides in elements, >= cols). */
+typedef struct {
+  const void* x;         /* rows x cols of `type`                                             */
+  const void* residual;  /* rows x cols of `type`, or NULL                                    */
+  const void* gain;      /* cols of gain_type, or NULL for ones                               */
+  void* h;               /* rows x cols of `type`: x + residual, or NULL; may be x or residual */
+  void* y;               /* rows x cols of `type`: the norm's output unquantized, or NULL; may
+                            be x or residual                                                  */
+  uint8_t* codes;        /* rows x cols E4M3FN codes, contiguous, or NULL (then scales too)   */
+  void* scales;          /* rows x ceil(cols / group) (one a row for group 0), contiguous     */
+  float* rstd;           /* rows, for the backward pass, or NULL                              */
+  int32_t* status;       /* set to FP4ROOT_ERR_NONFINITE where a row of x + residual or a group
+                            of outputs holds an infinity, or such a row a NaN, and left as it
+                            is otherwise; or NULL                                             */
+  int64_t rows, cols;    /* rows >= 0; cols in [1, 32768]                                     */
+  int64_t ld_x, ld_residual, ld_h, ld_y;
+  int32_t type;          /* FP4ROOT_FLOAT32, FP4ROOT_BFLOAT16 or FP4ROOT_FLOAT16              */
+  int32_t gain_type;     /* FP4ROOT_FLOAT32 or FP4ROOT_BFLOAT16                               */
+  int32_t group;         /* columns a scale covers: 32, 64 or 128 (the last group of a row may
+                            be shorter), or 0: the row                                        */
+  int32_t scale_type;    /* FP4ROOT_SCALE_*                                                   */
+  double eps;            /* > 0, finite                                                       */
+} fp4root_rmsnorm;
+
+/* h = round(x + residual) (x without a residual), rstd = fl32(1 / sqrt(sum h^2 / cols + eps))
+ * with the sum and the root in binary64, y = fl32(fl32(h rstd) gain), amax = max(max |y|,
+ * 2^-100) over a row or group, code = E4M3(fl32(y / s)) round to nearest even, with 1 / s as
+ * fl32(448 / amax) for FP32 scales and exact for E8M0.  A value is code * s.  A row with a NaN
+ * or an infinity in h has rstd and codes NaN; other rows are not touched by it. */
+int fp4root_rmsnorm_quantize(const fp4root_rmsnorm* args, void* stream);
+
+/* Workspace bytes fp4root_rmsnorm_backward needs, or 0 for a bad shape. */
+size_t fp4root_rmsnorm_backward_workspace(int64_t rows, int64_t cols);
+
+/* Gradients of y = (h rstd) gain (the rounding to 8 bits passed through as it is):
+ *   g = dy gain, xhat = h rstd, dx = rstd (g - xhat mean(g xhat)) + dh,
+ *   dgain = sum over rows of dy xhat.
+ * dx is the gradient of x and of the residual alike, rounded once; dgain is FP32 (what
+ * fp4root_qadamw_update reads) and its sum's order depends on the shape alone.
+ *   dy, h, dh (gradient that reaches h past the norm, or NULL), dx: rows x cols of `type`, row
+ *   strides ld_*; dx may be dy, h or dh; rstd: rows floats; gain: cols, or NULL for ones;
+ *   dgain: cols floats, or NULL (then ws may be NULL).  cols in [1, 32768]. */
+int fp4root_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh,
+                             int64_t ld_dh, const void* gain, const float* rstd, void* dx, int64_t ld_dx,
+                             float* dgain, int64_t rows, int64_t cols, int type, int gain_type, void* ws,
+                             size_t ws_bytes, void* stream);
+
 /* ---- helpers --------------------------------------------------------------- */
 
 /* The library's default per-step coefficients for a rows x cols matrix:

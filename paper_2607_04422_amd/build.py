@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfp4root.so")
 # sweeps of the device helpers over their ranges, loaded by tests only
 SWEEPS = os.path.join(HERE, "libfp4root_sweeps.so")
-SOURCES = ["quant.hip", "gemm_fp4.hip", "gemm_bf16.hip", "gemm_blaslt.cpp", "optim.hip", "api.cpp"]
+SOURCES = ["quant.hip", "gemm_fp4.hip", "gemm_bf16.hip", "gemm_blaslt.cpp", "optim.hip", "grads.hip", "rmsnorm.hip",
+           "api.cpp"]
 # the update product of the BF16 comparison path is a hipBLASLt GEMM
 LINK_LIBS = ["-L/opt/rocm/lib", "-lhipblaslt", "-Wl,-rpath,/opt/rocm/lib"]
 

@@ -8,6 +8,7 @@
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 #include <utility>
 #include <vector>
 
@@ -864,7 +865,7 @@ int check_momentum(const float* g, const float* m, int64_t batch, int64_t rows, 
 // The launches of fp4root_momentum_update (arguments already checked).
 int momentum_update_launch(const float* g, float* m, int64_t batch, int64_t rows, int64_t cols, uint8_t* codes,
                            uint8_t* scales, float* tensor_scale, float beta, uint32_t flags, uint64_t seed,
-                           int32_t step, void* ws, hipStream_t st) {
+                           int32_t step, const float* grad_scale, void* ws, hipStream_t st) {
   if (batch == 0) return FP4ROOT_OK;
   Carver cv(ws);
   uint32_t* status = cv.take<uint32_t>(1);
@@ -873,7 +874,7 @@ int momentum_update_launch(const float* g, float* m, int64_t batch, int64_t rows
   const float b1 = beta, b2 = 1.0f - beta;   // b2 = fl32(1 - beta)
   const uint32_t mask = sign_mask(seed, step), prev_mask = step > 0 ? sign_mask(seed, step - 1) : 0u;
   FP4R_TRY(launch_init(status, sc, batch, nullptr, 0, st));
-  FP4R_TRY(launch_mom_update(g, m, batch, rows, cols, codes, scales, tensor_scale, step > 0, prev_mask,
+  FP4R_TRY(launch_mom_update(g, grad_scale, m, batch, rows, cols, codes, scales, tensor_scale, step > 0, prev_mask,
                              mask, rot, b1, b2, sc, status, st));
   const Batch in{m, batch, rows, cols, cols, rows * cols};
   const QOut q{codes, scales, rows * cols / 2, rows * cols / 16};
@@ -891,11 +892,20 @@ int fp4root_momentum_update(const float* g, float* m, int64_t batch, int64_t row
                             uint8_t* codes, uint8_t* scales, float* tensor_scale, float beta,
                             uint32_t flags, uint64_t seed, int32_t step, void* ws, size_t ws_bytes,
                             void* stream) {
+  return fp4root_momentum_update_scaled(g, m, batch, rows, cols, codes, scales, tensor_scale, beta, flags, seed, step,
+                                        nullptr, ws, ws_bytes, stream);
+}
+
+int fp4root_momentum_update_scaled(const float* g, float* m, int64_t batch, int64_t rows, int64_t cols,
+                                   uint8_t* codes, uint8_t* scales, float* tensor_scale, float beta,
+                                   uint32_t flags, uint64_t seed, int32_t step, const float* grad_scale,
+                                   void* ws, size_t ws_bytes, void* stream) {
   const int rc = check_momentum(g, m, batch, rows, cols, codes, scales, tensor_scale, beta, flags, step);
   if (rc != FP4ROOT_OK) return rc;
+  if (!aligned(grad_scale, 4)) return FP4ROOT_ERR_INVALID_ARG;
   if (!ws || ws_bytes < fp4root_momentum_workspace(batch, rows, cols)) return FP4ROOT_ERR_WORKSPACE;
-  return momentum_update_launch(g, m, batch, rows, cols, codes, scales, tensor_scale, beta, flags, seed, step, ws,
-                                (hipStream_t)stream);
+  return momentum_update_launch(g, m, batch, rows, cols, codes, scales, tensor_scale, beta, flags, seed, step,
+                                grad_scale, ws, (hipStream_t)stream);
 }
 
 namespace {
@@ -927,11 +937,21 @@ int fp4root_qadamw_update(uint16_t* w, const float* g, float* m, int64_t n, uint
                           uint16_t* v_means, float lr, float wd, float beta1, float beta2, float eps,
                           uint32_t flags, uint64_t seed, int32_t step, void* ws, size_t ws_bytes,
                           void* stream) {
+  return fp4root_qadamw_update_scaled(w, g, m, n, m_codes, m_scales, m_tensor_scale, v_codes, v_scales, v_means, lr,
+                                      wd, beta1, beta2, eps, flags, seed, step, nullptr, ws, ws_bytes, stream);
+}
+
+int fp4root_qadamw_update_scaled(uint16_t* w, const float* g, float* m, int64_t n, uint8_t* m_codes,
+                                 uint8_t* m_scales, float* m_tensor_scale, uint8_t* v_codes,
+                                 uint16_t* v_scales, uint16_t* v_means, float lr, float wd, float beta1,
+                                 float beta2, float eps, uint32_t flags, uint64_t seed, int32_t step,
+                                 const float* grad_scale, void* ws, size_t ws_bytes, void* stream) {
   int64_t vr = 0, vc = 0;
   if (!flat_view(n, vr, vc)) return FP4ROOT_ERR_SHAPE;
   if (step < 0 || !w || !g || !m_codes || !m_scales || !m_tensor_scale || !v_codes || !v_scales || !v_means)
     return FP4ROOT_ERR_INVALID_ARG;
-  if (!aligned(w, 16) || !aligned(g, 16) || (m && !aligned(m, 16)) || !aligned(m_codes, 8) || !aligned(v_codes, 8))
+  if (!aligned(w, 16) || !aligned(g, 16) || (m && !aligned(m, 16)) || !aligned(m_codes, 8) || !aligned(v_codes, 8) ||
+      !aligned(grad_scale, 4))
     return FP4ROOT_ERR_INVALID_ARG;
   // the second pass reads g again: the first-moment output may not overlap it
   if (m && (const char*)m < (const char*)(g + n) && (const char*)g < (const char*)(m + n))
@@ -956,7 +976,7 @@ int fp4root_qadamw_update(uint16_t* w, const float* g, float* m, int64_t n, uint
   FP4R_TRY(launch_init(status, sc, 1, nullptr, 0, st));
   // pass 1: first moment (read only), its rotated amax, second moment and weights
   QAdamWLaunch q;
-  q.w = w; q.g = g; q.m_out = m; q.mcodes = m_codes; q.mscales = m_scales; q.m_prev_sg = m_tensor_scale;
+  q.w = w; q.g = g; q.grad_scale = grad_scale; q.m_out = m; q.mcodes = m_codes; q.mscales = m_scales; q.m_prev_sg = m_tensor_scale;
   q.b1 = beta1;
   q.c1m = 1.0f - beta1;
   q.sc = sc;
@@ -978,7 +998,7 @@ int fp4root_qadamw_update(uint16_t* w, const float* g, float* m, int64_t n, uint
   FP4R_TRY(launch_qadamw(q, st));
   // pass 2: the first moment re-derived and encoded in place
   const uint64_t key = splitmix64(seed ^ 0x5352ull, (uint64_t)step + 1);
-  FP4R_TRY(launch_mom_encode(g, m_codes, m_scales, n, step > 0, prev_mask, mask, rot, ad,
+  FP4R_TRY(launch_mom_encode(g, grad_scale, m_codes, m_scales, n, step > 0, prev_mask, mask, rot, ad,
                              flags & FP4ROOT_F_STOCHASTIC, beta1, 1.0f - beta1, sc, m_tensor_scale, key, st));
   return FP4ROOT_OK;
 }
@@ -1064,7 +1084,13 @@ void root_chunk(const fp4root_param* params, int64_t count, int64_t first, const
 
 int fp4root_root_step(const fp4root_param* params, int64_t count, const fp4root_root_config* rc,
                       const fp4root_ns_config* ns, void* ws, size_t ws_bytes, void* stream) {
-  if (count < 0 || (count > 0 && !params) || !rc || !ns) return FP4ROOT_ERR_INVALID_ARG;
+  return fp4root_root_step_scaled(params, count, rc, ns, nullptr, ws, ws_bytes, stream);
+}
+
+int fp4root_root_step_scaled(const fp4root_param* params, int64_t count, const fp4root_root_config* rc,
+                             const fp4root_ns_config* ns, const float* grad_scale, void* ws, size_t ws_bytes,
+                             void* stream) {
+  if (count < 0 || (count > 0 && !params) || !rc || !ns || !aligned(grad_scale, 4)) return FP4ROOT_ERR_INVALID_ARG;
   // every argument is checked before the first launch, so an error leaves every
   // parameter's state unchanged
   for (int64_t i = 0; i < count; ++i) {
@@ -1099,7 +1125,7 @@ int fp4root_root_step(const fp4root_param* params, int64_t count, const fp4root_
     root_chunk(params, count, i, *rc, ch);
     FP4R_TRY(launch_init(i == 0 ? status : nullptr, sc, ch.count, nullptr, 0, st));
     FP4R_TRY(launch_root_momentum(ch, rc->step > 0, mf & FP4ROOT_F_HADAMARD, mf & FP4ROOT_F_ADAPTIVE46,
-                                  mf & FP4ROOT_F_STOCHASTIC, b1, b2, sc, status, st));
+                                  mf & FP4ROOT_F_STOCHASTIC, b1, b2, grad_scale, sc, status, st));
   }
   const int rc2 = orthogonalize_launch(mats.data(), count, ns, ws, false, st);
   if (rc2 != FP4ROOT_OK) return rc2;
@@ -1347,6 +1373,330 @@ int fp4root_orthogonalize(const fp4root_matrix* mats, int64_t count, const fp4ro
   if (rc != FP4ROOT_OK) return rc;
   if (!ws || ws_bytes < orthogonalize_ws_size(mats, count, cfg)) return FP4ROOT_ERR_WORKSPACE;
   return orthogonalize_launch(mats, count, cfg, ws, true, (hipStream_t)stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Gradient norm, clipping and the root-mean-square norm.
+
+namespace {
+// Rows of bytes that a call reads or writes.
+struct Span {
+  uintptr_t p;
+  int64_t rows, row, ld;   // bytes
+  uintptr_t end() const { return p + (uintptr_t)((rows - 1) * ld + row); }
+};
+// Whether two spans have a byte in common.  Views of different columns of one matrix do not;
+// rows of different strides whose extents meet are taken to.
+bool meet(Span a, Span b) {
+  if (a.rows <= 0 || b.rows <= 0 || a.row <= 0 || b.row <= 0) return false;
+  if (a.end() <= b.p || b.end() <= a.p) return false;
+  if (a.rows == 1) a.ld = b.ld;
+  if (b.rows == 1) b.ld = a.ld;
+  if (a.ld != b.ld || (a.rows == 1 && b.rows == 1)) return true;
+  const int64_t ld = a.ld;
+  int64_t d = (int64_t)((intptr_t)b.p - (intptr_t)a.p) % ld;
+  if (d < 0) d += ld;
+  return a.row > ld || b.row > ld || d < a.row || d + b.row > ld;
+}
+bool same(const Span& a, const Span& b) { return a.p == b.p && a.row == b.row && (a.ld == b.ld || a.rows == 1); }
+
+constexpr int64_t kMaxTensors = int64_t(1) << 20;
+int64_t type_size(int32_t t) { return t == FP4ROOT_FLOAT32 ? 4 : 2; }
+bool type_ok(int32_t t) { return t == FP4ROOT_FLOAT32 || t == FP4ROOT_BFLOAT16 || t == FP4ROOT_FLOAT16; }
+Span span(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
+  return Span{(uintptr_t)p, rows, cols * size, ld * size};
+}
+
+int check_tensors(const fp4root_tensor* t, int64_t count, bool out) {
+  if (count < 0 || count > kMaxTensors || (count > 0 && !t)) return FP4ROOT_ERR_INVALID_ARG;
+  for (int64_t i = 0; i < count; ++i) {
+    if (!type_ok(t[i].in_type) || (out && !type_ok(t[i].out_type))) return FP4ROOT_ERR_INVALID_ARG;
+    if (t[i].rows < 0 || t[i].cols < 0) return FP4ROOT_ERR_SHAPE;
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    if (t[i].rows > kMaxElems || t[i].cols > kMaxElems / t[i].rows) return FP4ROOT_ERR_SHAPE;
+    if (t[i].rows > 1 && (t[i].ld_in < t[i].cols || t[i].ld_in > kMaxLd ||
+                          (out && (t[i].ld_out < t[i].cols || t[i].ld_out > kMaxLd))))
+      return FP4ROOT_ERR_SHAPE;
+    if (t[i].rows > 1 && (t[i].rows - 1) > (int64_t(1) << 40) / std::max(t[i].ld_in, out ? t[i].ld_out : 1))
+      return FP4ROOT_ERR_SHAPE;
+    if (!t[i].in || !aligned(t[i].in, (size_t)type_size(t[i].in_type))) return FP4ROOT_ERR_INVALID_ARG;
+    if (out && (!t[i].out || !aligned(t[i].out, (size_t)type_size(t[i].out_type)))) return FP4ROOT_ERR_INVALID_ARG;
+  }
+  return FP4ROOT_OK;
+}
+
+// Workgroups run side by side, so no output may meet another tensor's input or output, nor its
+// own input unless it is that very tensor.
+bool outputs_apart(const fp4root_tensor* t, int64_t count) {
+  struct Item {
+    Span s;
+    int64_t i;
+    bool out;
+  };
+  std::vector<Item> items;
+  items.reserve((size_t)(2 * count));
+  for (int64_t i = 0; i < count; ++i) {
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    const Span in = span(t[i].in, t[i].rows, t[i].cols, t[i].rows > 1 ? t[i].ld_in : t[i].cols, type_size(t[i].in_type));
+    const Span o = span(t[i].out, t[i].rows, t[i].cols, t[i].rows > 1 ? t[i].ld_out : t[i].cols, type_size(t[i].out_type));
+    const bool in_place = same(in, o) && t[i].in_type == t[i].out_type;
+    if (!in_place && meet(in, o)) return false;
+    if (!in_place) items.push_back(Item{in, i, false});
+    items.push_back(Item{o, i, true});
+  }
+  std::sort(items.begin(), items.end(), [](const Item& a, const Item& b) { return a.s.p < b.s.p; });
+  std::vector<size_t> open;   // items whose extents reach the current start
+  for (size_t k = 0; k < items.size(); ++k) {
+    size_t kept = 0;
+    for (const size_t o : open) {
+      if (items[o].s.end() <= items[k].s.p) continue;
+      open[kept++] = o;
+      if ((items[o].out || items[k].out) && items[o].i != items[k].i && meet(items[o].s, items[k].s)) return false;
+    }
+    open.resize(kept);
+    open.push_back(k);
+  }
+  return true;
+}
+
+// The tensor as the kernels walk it: contiguous ones as a row, cut into parts of 2^shift
+// vectors, 64 KB at least, and into at most 1024 of them.
+int64_t grad_ref(const fp4root_tensor& t, bool out, GradRef& r, uint8_t& shift) {
+  r = GradRef{t.in, out ? t.out : nullptr, t.rows, t.cols, t.ld_in, out ? t.ld_out : 0, 0};
+  if (t.rows == 0 || t.cols == 0) {
+    r.rows = 1;
+    r.cols = 0;
+  } else if (t.rows > 1 && t.ld_in == t.cols && (!out || t.ld_out == t.cols)) {
+    r.rows = 1;
+    r.cols = t.rows * t.cols;
+  }
+  const int64_t ve = 16 / type_size(t.in_type);
+  r.vectors = r.rows * ((r.cols + ve - 1) / ve);
+  int s = 12;
+  while (r.vectors > int64_t(1024) << s) ++s;
+  shift = (uint8_t)s;
+  return std::max<int64_t>(1, (r.vectors + (int64_t(1) << s) - 1) >> s);
+}
+
+// Calls launch(chunk, first part, first tensor) for runs of up to kMaxGradChunk tensors.
+template <class F>
+int each_grad_chunk(const fp4root_tensor* t, int64_t count, bool out, F launch) {
+  int64_t part = 0;
+  for (int64_t i0 = 0; i0 < count; i0 += kMaxGradChunk) {
+    GradChunk ch;
+    ch.count = (int)std::min<int64_t>(kMaxGradChunk, count - i0);
+    int64_t end = 0;
+    for (int k = 0; k < ch.count; ++k) {
+      const fp4root_tensor& g = t[i0 + k];
+      end += grad_ref(g, out, ch.t[k], ch.shift[k]);
+      ch.end[k] = (uint32_t)end;
+      ch.type[k] = (uint8_t)(g.in_type | (out ? g.out_type : 0) << 2);
+    }
+    FP4R_TRY(launch(ch, (uint32_t)part, (uint32_t)i0));
+    part += end;
+  }
+  return FP4ROOT_OK;
+}
+
+int64_t grad_parts(const fp4root_tensor* t, int64_t count) {
+  int64_t parts = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    GradRef r;
+    uint8_t shift;
+    parts += grad_ref(t[i], false, r, shift);
+  }
+  return parts;
+}
+
+size_t carve_grad_norm(void* base, int64_t count, int64_t parts, GradNormWs& w) {
+  Carver cv(base);
+  w.status = cv.take<uint32_t>(1);
+  w.ticket = cv.take<uint32_t>(1);
+  w.first = cv.take<uint32_t>((size_t)count);
+  w.sums = cv.take<double>((size_t)count);
+  w.parts = cv.take<double>((size_t)parts);
+  return cv.off;
+}
+
+int check_clip(int kind, double max_norm, double eps, const void* total, const void* result) {
+  if (kind != FP4ROOT_NORM_L2 && kind != FP4ROOT_NORM_MAX) return FP4ROOT_ERR_INVALID_ARG;
+  if (!(max_norm > 0.0) || !(eps >= 0.0) || !std::isfinite(eps)) return FP4ROOT_ERR_INVALID_ARG;
+  if (!total || !aligned(total, 8) || !result || !aligned(result, 4)) return FP4ROOT_ERR_INVALID_ARG;
+  return FP4ROOT_OK;
+}
+}  // namespace
+
+extern "C" {
+
+size_t fp4root_grad_norm_workspace(const fp4root_tensor* tensors, int64_t count) {
+  if (check_tensors(tensors, count, false) != FP4ROOT_OK) return 0;
+  GradNormWs w;
+  return carve_grad_norm(nullptr, count, grad_parts(tensors, count), w);
+}
+
+int fp4root_grad_norm(const fp4root_tensor* tensors, int64_t count, int kind, double max_norm, double eps,
+                      double* total, float* norms, float* result, void* ws, size_t ws_bytes, void* stream) {
+  FP4R_TRY_RC(check_tensors(tensors, count, false));
+  FP4R_TRY_RC(check_clip(kind, max_norm, eps, total, result));
+  if (!aligned(norms, 4)) return FP4ROOT_ERR_INVALID_ARG;
+  const int64_t parts = grad_parts(tensors, count);
+  GradNormWs w;
+  if (!ws || !aligned(ws, 8) || ws_bytes < carve_grad_norm(ws, count, parts, w)) return FP4ROOT_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  const bool max = kind == FP4ROOT_NORM_MAX;
+  FP4R_TRY_RC(each_grad_chunk(tensors, count, false, [&](const GradChunk& ch, uint32_t part, uint32_t first) {
+    return launch_grad_parts(ch, w, part, first, max, st);
+  }));
+  FP4R_TRY(launch_grad_total(w, (uint32_t)count, (uint32_t)parts, max, max_norm, eps, total, norms, result, st));
+  return FP4ROOT_OK;
+}
+
+int fp4root_clip_coef(const double* total, int kind, double max_norm, double eps, float* result, void* stream) {
+  FP4R_TRY_RC(check_clip(kind, max_norm, eps, total, result));
+  FP4R_TRY(launch_clip_coef(total, kind == FP4ROOT_NORM_MAX, max_norm, eps, result, (hipStream_t)stream));
+  return FP4ROOT_OK;
+}
+
+int fp4root_clip_grads(const fp4root_tensor* tensors, int64_t count, const float* coef, void* stream) {
+  FP4R_TRY_RC(check_tensors(tensors, count, true));
+  if (!coef || !aligned(coef, 4)) return FP4ROOT_ERR_INVALID_ARG;
+  try {
+    if (!outputs_apart(tensors, count)) return FP4ROOT_ERR_INVALID_ARG;
+  } catch (const std::bad_alloc&) {
+    return FP4ROOT_ERR_HIP;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  return each_grad_chunk(tensors, count, true,
+                         [&](const GradChunk& ch, uint32_t, uint32_t) { return launch_grad_scale(ch, coef, st); });
+}
+
+namespace {
+bool norm_shape_ok(int64_t rows, int64_t cols) {
+  return rows >= 0 && cols >= 1 && cols <= kMaxNormCols && rows <= kMaxElems / cols;
+}
+bool ld_ok(int64_t rows, int64_t cols, int64_t ld) {
+  return rows <= 1 || (ld >= cols && ld <= kMaxLd && rows - 1 <= (int64_t(1) << 40) / ld);
+}
+bool gain_ok(const void* gain, int32_t type) {
+  return !gain || ((type == FP4ROOT_FLOAT32 || type == FP4ROOT_BFLOAT16) && aligned(gain, (size_t)type_size(type)));
+}
+// Rows per launch: a grid of a workgroup of up to 1024 threads a row stays below 2^32 threads.
+constexpr int64_t kNormRows = int64_t(1) << 21;
+}  // namespace
+
+int fp4root_rmsnorm_quantize(const fp4root_rmsnorm* args, void* stream) {
+  if (!args) return FP4ROOT_ERR_INVALID_ARG;
+  const fp4root_rmsnorm& a = *args;
+  if (!type_ok(a.type) || !gain_ok(a.gain, a.gain_type)) return FP4ROOT_ERR_INVALID_ARG;
+  if (a.group != 0 && a.group != 32 && a.group != 64 && a.group != 128) return FP4ROOT_ERR_INVALID_ARG;
+  if (a.scale_type != FP4ROOT_SCALE_FP32 && a.scale_type != FP4ROOT_SCALE_E8M0) return FP4ROOT_ERR_INVALID_ARG;
+  if (!(a.eps > 0.0) || !std::isfinite(a.eps)) return FP4ROOT_ERR_INVALID_ARG;
+  if (!norm_shape_ok(a.rows, a.cols)) return FP4ROOT_ERR_SHAPE;
+  if (a.rows == 0) return FP4ROOT_OK;
+  const int64_t size = type_size(a.type), groups = a.group ? (a.cols + a.group - 1) / a.group : 1;
+  const bool e8m0 = a.scale_type == FP4ROOT_SCALE_E8M0;
+  if (!a.x || (!a.codes) != (!a.scales) || (!a.h && !a.y && !a.codes && !a.rstd)) return FP4ROOT_ERR_INVALID_ARG;
+  if (!aligned(a.x, size) || !aligned(a.residual, size) || !aligned(a.h, size) || !aligned(a.y, size) ||
+      !aligned(a.scales, e8m0 ? 1 : 4) || !aligned(a.rstd, 4) || !aligned(a.status, 4))
+    return FP4ROOT_ERR_INVALID_ARG;
+  if (!ld_ok(a.rows, a.cols, a.ld_x) || (a.residual && !ld_ok(a.rows, a.cols, a.ld_residual)) ||
+      (a.h && !ld_ok(a.rows, a.cols, a.ld_h)) || (a.y && !ld_ok(a.rows, a.cols, a.ld_y)))
+    return FP4ROOT_ERR_SHAPE;
+  // a row's threads read all of it before they write: an output may be an input, but meet none
+  const auto mat = [&](const void* p, int64_t ld) { return span(p, p ? a.rows : 0, a.cols, a.rows > 1 ? ld : a.cols, size); };
+  const Span in[3] = {mat(a.x, a.ld_x), mat(a.residual, a.ld_residual),
+                      span(a.gain, a.gain ? 1 : 0, a.cols, a.cols, type_size(a.gain_type))};
+  const Span out[6] = {mat(a.h, a.ld_h), mat(a.y, a.ld_y), span(a.codes, a.codes ? 1 : 0, a.rows * a.cols, 0, 1),
+                       span(a.scales, a.scales ? 1 : 0, a.rows * groups, 0, e8m0 ? 1 : 4),
+                       span(a.rstd, a.rstd ? 1 : 0, a.rows, 0, 4), span(a.status, a.status ? 1 : 0, 1, 0, 4)};
+  for (int o = 0; o < 6; ++o) {
+    for (int i = 0; i < 3; ++i)
+      if (!(o < 2 && i < 2 && same(out[o], in[i])) && meet(out[o], in[i])) return FP4ROOT_ERR_INVALID_ARG;
+    for (int q = 0; q < o; ++q)
+      if (meet(out[o], out[q])) return FP4ROOT_ERR_INVALID_ARG;
+  }
+  for (int64_t r0 = 0; r0 < a.rows; r0 += kNormRows) {
+    const auto at = [&](const void* p, int64_t ld) { return p ? (char*)p + r0 * ld * size : nullptr; };
+    RmsArgs k{};
+    k.x = at(a.x, a.ld_x);
+    k.r = at(a.residual, a.ld_residual);
+    k.h = at(a.h, a.ld_h);
+    k.y = at(a.y, a.ld_y);
+    k.gain = a.gain;
+    k.codes = a.codes ? a.codes + r0 * a.cols : nullptr;
+    k.scales = a.scales ? (char*)a.scales + r0 * groups * (e8m0 ? 1 : 4) : nullptr;
+    k.rstd = a.rstd ? a.rstd + r0 : nullptr;
+    k.status = a.status;
+    k.rows = std::min(kNormRows, a.rows - r0);
+    k.ld_x = a.ld_x;
+    k.ld_r = a.ld_residual;
+    k.ld_h = a.ld_h;
+    k.ld_y = a.ld_y;
+    k.cols = (int32_t)a.cols;
+    k.group = a.group;
+    k.groups = (int32_t)groups;
+    k.type = a.type;
+    k.gain_f32 = a.gain_type == FP4ROOT_FLOAT32;
+    k.e8m0 = e8m0;
+    k.eps = a.eps;
+    FP4R_TRY(launch_rmsnorm(k, (hipStream_t)stream));
+  }
+  return FP4ROOT_OK;
+}
+
+size_t fp4root_rmsnorm_backward_workspace(int64_t rows, int64_t cols) {
+  if (!norm_shape_ok(rows, cols)) return 0;
+  return std::max<size_t>(kAlign, (size_t)(rms_bwd_groups(rows, cols) * cols) * sizeof(float));
+}
+
+int fp4root_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh,
+                             int64_t ld_dh, const void* gain, const float* rstd, void* dx, int64_t ld_dx,
+                             float* dgain, int64_t rows, int64_t cols, int type, int gain_type, void* ws,
+                             size_t ws_bytes, void* stream) {
+  if (!type_ok(type) || !gain_ok(gain, gain_type)) return FP4ROOT_ERR_INVALID_ARG;
+  if (!norm_shape_ok(rows, cols)) return FP4ROOT_ERR_SHAPE;
+  const int64_t size = type_size(type);
+  if (rows > 0 && (!dy || !h || !rstd || !dx)) return FP4ROOT_ERR_INVALID_ARG;
+  if (!aligned(dy, size) || !aligned(h, size) || !aligned(dh, size) || !aligned(dx, size) || !aligned(rstd, 4) ||
+      !aligned(dgain, 4))
+    return FP4ROOT_ERR_INVALID_ARG;
+  if (!ld_ok(rows, cols, ld_dy) || !ld_ok(rows, cols, ld_h) || (dh && !ld_ok(rows, cols, ld_dh)) ||
+      !ld_ok(rows, cols, ld_dx))
+    return FP4ROOT_ERR_SHAPE;
+  const auto mat = [&](const void* p, int64_t ld) { return span(p, p ? rows : 0, cols, rows > 1 ? ld : cols, size); };
+  const size_t need = dgain ? fp4root_rmsnorm_backward_workspace(rows, cols) : 0;
+  const Span in[5] = {mat(dy, ld_dy), mat(h, ld_h), mat(dh, ld_dh),
+                      span(gain, gain ? 1 : 0, cols, 0, type_size(gain_type)), span(rstd, rstd ? 1 : 0, rows, 0, 4)};
+  const Span out[3] = {mat(dx, ld_dx), span(dgain, dgain ? 1 : 0, cols, 0, 4),
+                       span(ws, dgain && ws ? 1 : 0, (int64_t)need, 0, 1)};
+  for (int o = 0; o < 3; ++o) {
+    for (int i = 0; i < 5; ++i)
+      if (!(o == 0 && i < 3 && same(out[o], in[i])) && meet(out[o], in[i])) return FP4ROOT_ERR_INVALID_ARG;
+    for (int q = 0; q < o; ++q)
+      if (meet(out[o], out[q])) return FP4ROOT_ERR_INVALID_ARG;
+  }
+  if (dgain && (!ws || !aligned(ws, 4) || ws_bytes < need)) return FP4ROOT_ERR_WORKSPACE;
+  RmsBwdArgs k{};
+  k.dy = dy;
+  k.h = h;
+  k.dh = dh;
+  k.gain = gain;
+  k.rstd = rstd;
+  k.dx = dx;
+  k.dgain = dgain;
+  k.partial = (float*)ws;
+  k.rows = rows;
+  k.ld_dy = ld_dy;
+  k.ld_h = ld_h;
+  k.ld_dh = ld_dh;
+  k.ld_dx = ld_dx;
+  k.cols = (int32_t)cols;
+  k.type = type;
+  k.gain_f32 = gain_type == FP4ROOT_FLOAT32;
+  FP4R_TRY(launch_rmsnorm_backward(k, (hipStream_t)stream));
+  return FP4ROOT_OK;
 }
 
 }  // extern "C"

@@ -482,6 +482,14 @@ FP4R_DEV double recip64(float b) {
   return __builtin_fma(x, __builtin_fma(e, e, e), x);
 }
 
+// Gradients times the clipping coefficient, where there is one (uniform).
+FP4R_DEV void scale16(float (&x)[16], const float* grad_scale) {
+  if (!grad_scale) return;
+  const float s = *grad_scale;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] *= s;
+}
+
 // The first-moment update of one 16-element block at flat offset e0: decode of the
 // previous state (q s exact, times its tensor scale with one rounding, then the
 // inverse rotation) when has_prev, then m = fl32(b1 m_hat + b2 g) with exact

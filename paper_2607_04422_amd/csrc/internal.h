@@ -9,6 +9,7 @@ namespace fp4r {
 
 // Device status bits (kept in the first word of every workspace).
 constexpr uint32_t kStatusNonFinite = 1u;
+constexpr int32_t kErrNonFinite = -4;   // FP4ROOT_ERR_NONFINITE, for status words that callers read
 
 // ---------------------------------------------------------------------------
 // Matrix lists for the stages that read caller matrices (clipping, copies): up to
@@ -304,8 +305,9 @@ hipError_t launch_encode_sr(const Batch& in, uint32_t sign_mask, bool rotate, bo
 // First-moment update of a batch of contiguous rows x cols matrices (matrix
 // stride rows*cols): m = fl32(b1 decode(previous state) + b2 g) (previous state
 // read only when has_prev, decoded with prev_mask), amax of m rotated with `mask`
-// into amax slot 0 of sc[b]; non-finite g sets the status word.
-hipError_t launch_mom_update(const float* g, float* m, int64_t batch, int64_t rows, int64_t cols,
+// into amax slot 0 of sc[b]; non-finite g sets the status word.  grad_scale (here and below):
+// null, or a device scalar that multiplies every element of g as it is read.
+hipError_t launch_mom_update(const float* g, const float* grad_scale, float* m, int64_t batch, int64_t rows, int64_t cols,
                              const uint8_t* codes, const uint8_t* scales, const float* prev_sg,
                              bool has_prev, uint32_t prev_mask, uint32_t mask, bool rotate, float b1,
                              float b2, MatScalars* sc, uint32_t* status, hipStream_t st);
@@ -348,14 +350,14 @@ __device__ inline int root_param(const RootChunk& ch, uint32_t wg, uint32_t& loc
 // launch_mom_update, then launch_encode_sr (or launch_encode) of each parameter's m;
 // parameter i of the chunk uses sc[i].
 hipError_t launch_root_momentum(const RootChunk& ch, bool has_prev, bool rotate, bool adaptive, bool sr, float b1,
-                                float b2, MatScalars* sc, uint32_t* status, hipStream_t st);
+                                float b2, const float* grad_scale, MatScalars* sc, uint32_t* status, hipStream_t st);
 // launch_apply_update of each parameter (O = m).
 hipError_t launch_root_apply(const RootChunk& ch, float c1, hipStream_t st);
 
 // Second pass of a quantized-state AdamW step on a flat parameter of n elements:
 // re-derive m_t from g and the unchanged previous first-moment state and encode it
 // in place (stochastically when sr), tensor scale from amax slot 0 of sc[0].
-hipError_t launch_mom_encode(const float* g, uint8_t* codes, uint8_t* scales, int64_t n, bool has_prev,
+hipError_t launch_mom_encode(const float* g, const float* grad_scale, uint8_t* codes, uint8_t* scales, int64_t n, bool has_prev,
                              uint32_t prev_mask, uint32_t mask, bool rotate, bool adaptive, bool sr, float b1,
                              float b2, MatScalars* sc, float* tensor_scale, uint64_t sr_key, hipStream_t st);
 
@@ -367,6 +369,7 @@ hipError_t launch_mom_encode(const float* g, uint8_t* codes, uint8_t* scales, in
 struct QAdamWLaunch {
   uint16_t* w;
   const float* g;
+  const float* grad_scale;
   float* m_out;
   const uint8_t* mcodes;
   const uint8_t* mscales;
@@ -383,6 +386,65 @@ struct QAdamWLaunch {
   uint32_t* status;
 };
 hipError_t launch_qadamw(const QAdamWLaunch& p, hipStream_t st);
+
+// ---------------------------------------------------------------------------
+// Gradient lists (grads.hip): up to kMaxGradChunk tensors a launch, by value.
+constexpr int kMaxGradChunk = 64;
+struct GradRef {
+  const void* in;
+  void* out;
+  int64_t rows, cols;      // one row where the tensor is contiguous
+  int64_t ld_in, ld_out;
+  int64_t vectors;         // of 16 bytes of the input: rows * ceil(cols / elements in 16 bytes)
+};
+struct GradChunk {
+  GradRef t[kMaxGradChunk];
+  uint32_t end[kMaxGradChunk];    // parts up to and with tensor i
+  uint8_t shift[kMaxGradChunk];   // log2 of the vectors in a part
+  uint8_t type[kMaxGradChunk];    // input type | output type << 2
+  int count;
+};
+// Workspace of the norm: the first part of each tensor, and the sums of tensors and parts.
+struct GradNormWs {
+  uint32_t *status, *ticket, *first;
+  double *sums, *parts;
+};
+static_assert(sizeof(GradChunk) + sizeof(GradNormWs) + 8 <= 4096, "a launch's arguments");
+hipError_t launch_grad_parts(const GradChunk& ch, const GradNormWs& ws, uint32_t first_part, uint32_t first_tensor,
+                             bool max, hipStream_t st);
+hipError_t launch_grad_total(const GradNormWs& ws, uint32_t count, uint32_t parts, bool max, double max_norm, double eps,
+                             double* total, float* norms, float* result, hipStream_t st);
+hipError_t launch_clip_coef(const double* total, bool max, double max_norm, double eps, float* result, hipStream_t st);
+hipError_t launch_grad_scale(const GradChunk& ch, const float* coef, hipStream_t st);
+
+// ---------------------------------------------------------------------------
+// Root-mean-square norm (rmsnorm.hip).
+constexpr int64_t kMaxNormCols = 32768;   // a row stays in the registers of one workgroup
+struct RmsArgs {
+  const void *x, *r, *gain;
+  void *h, *y, *scales;
+  uint8_t* codes;
+  float* rstd;
+  int32_t* status;
+  int64_t rows, ld_x, ld_r, ld_h, ld_y;
+  int32_t cols, group, groups;   // group: columns a scale covers, 0 for the row; groups: scales a row
+  int32_t type, gain_f32, e8m0;
+  double eps;
+};
+hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st);
+
+struct RmsBwdArgs {
+  const void *dy, *h, *dh, *gain;
+  const float* rstd;
+  void* dx;
+  float* dgain;
+  float* partial;          // rms_bwd_groups(rows, cols) rows of cols
+  int64_t rows, ld_dy, ld_h, ld_dh, ld_dx;
+  int32_t cols, type, gain_f32;
+};
+// Workgroups of the first pass, each with one partial row of the gain's gradient.
+int64_t rms_bwd_groups(int64_t rows, int64_t cols);
+hipError_t launch_rmsnorm_backward(const RmsBwdArgs& a, hipStream_t st);
 
 // Both quantisations of X (m x n, row stride n) from one read: qX along n into
 // qx (slot_n), qXt along m into qxt (slot_m, stored transposed).

@@ -72,6 +72,7 @@ hipError_t launch_apply_update(uint16_t* w, const float* o, int64_t count, float
 struct QAdamWArgs {
   uint16_t* w;
   const float* g;
+  const float* grad_scale; // optional: multiplies g
   float* m_out;            // optional: this step's binary32 first moment
   const uint8_t* mcodes;   // previous first-moment state (read only here)
   const uint8_t* mscales;
@@ -107,6 +108,7 @@ __global__ __launch_bounds__(256) void k_qadamw(QAdamWArgs a) {
       g[4 * q] = x.x; g[4 * q + 1] = x.y; g[4 * q + 2] = x.z; g[4 * q + 3] = x.w;
     }
   }
+  scale16(g, a.grad_scale);
   const bool ok = finite16(g);
   if (live && !ok) atomicOr(a.status, kStatusNonFinite);
   // this step's first moment, and the rotated amax of it for the second pass
@@ -235,7 +237,7 @@ __global__ __launch_bounds__(256) void k_qadamw(QAdamWArgs a) {
 
 hipError_t launch_qadamw(const QAdamWLaunch& p, hipStream_t st) {
   QAdamWArgs a;
-  a.w = p.w; a.g = p.g; a.m_out = p.m_out; a.mcodes = p.mcodes; a.mscales = p.mscales; a.m_prev_sg = p.m_prev_sg;
+  a.w = p.w; a.g = p.g; a.grad_scale = p.grad_scale; a.m_out = p.m_out; a.mcodes = p.mcodes; a.mscales = p.mscales; a.m_prev_sg = p.m_prev_sg;
   a.b1 = p.b1; a.c1m = p.c1m; a.sc = p.sc;
   a.vcodes = p.vcodes; a.vscales = p.vscales; a.vmeans = p.vmeans;
   a.nblk = p.n / 16;

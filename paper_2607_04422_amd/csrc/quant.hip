@@ -1422,7 +1422,7 @@ hipError_t launch_encode_sr(const Batch& in, uint32_t sign_mask, bool rotate, bo
 // inverse rotation), forms m = fl32(b1 m_hat + b2 g) (exact products, one binary64
 // rounding, then binary32), writes m and records the amax of m rotated with
 // `mask` (the tensor scale of the next state) in amax slot 0.
-FP4R_DEV void mom_update_block(const float* g, float* m, int64_t e0, bool in, const uint8_t* codes,
+FP4R_DEV void mom_update_block(const float* g, const float* grad_scale, float* m, int64_t e0, bool in, const uint8_t* codes,
                                const uint8_t* scales, float prev_sg, int has_prev, uint32_t prev_mask,
                                uint32_t mask, int rotate, float b1, float b2, MatScalars* sc, uint32_t wg,
                                uint32_t* status) {
@@ -1436,6 +1436,7 @@ FP4R_DEV void mom_update_block(const float* g, float* m, int64_t e0, bool in, co
       const float4 v = gp[q];
       x[4 * q] = v.x; x[4 * q + 1] = v.y; x[4 * q + 2] = v.z; x[4 * q + 3] = v.w;
     }
+    scale16(x, grad_scale);
     const bool ok = finite16(x);
     if (!ok) atomicOr(status, kStatusNonFinite);
     float mv[16];
@@ -1460,14 +1461,14 @@ FP4R_DEV void mom_update_block(const float* g, float* m, int64_t e0, bool in, co
   }
 }
 
-__global__ __launch_bounds__(256) void k_mom_update(const float* g, float* m, int64_t rows, int64_t cols,
+__global__ __launch_bounds__(256) void k_mom_update(const float* g, const float* grad_scale, float* m, int64_t rows, int64_t cols,
                                                     const uint8_t* codes, const uint8_t* scales,
                                                     const float* prev_sg, int has_prev, uint32_t prev_mask,
                                                     uint32_t mask, int rotate, float b1, float b2,
                                                     MatScalars* sc, uint32_t* status) {
   const int64_t b = blockIdx.y;
   const int64_t blk = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  mom_update_block(g, m, b * rows * cols + blk * 16, blk < rows * cols / 16, codes, scales,
+  mom_update_block(g, grad_scale, m, b * rows * cols + blk * 16, blk < rows * cols / 16, codes, scales,
                    has_prev ? prev_sg[b] : 0.0f, has_prev, prev_mask, mask, rotate, b1, b2, &sc[b], blockIdx.x,
                    status);
 }
@@ -1476,12 +1477,12 @@ __global__ __launch_bounds__(256) void k_mom_update(const float* g, float* m, in
 // to kMaxRootChunk of them: small parameters are bound by the launches (12 parameters of 64
 // to 256 K elements: 188 us in 49 launches of their own, 25 in 4).
 __global__ __launch_bounds__(256) void k_root_mom_update(RootChunk ch, int has_prev, int rotate, float b1, float b2,
-                                                         MatScalars* sc, uint32_t* status) {
+                                                         const float* grad_scale, MatScalars* sc, uint32_t* status) {
   uint32_t wg;
   const int i = root_param(ch, blockIdx.x, wg);
   const RootRef& p = ch.p[i];
   const int64_t blk = (int64_t)wg * 256 + threadIdx.x;
-  mom_update_block(p.g, p.m, blk * 16, blk < p.nblk, p.codes, p.scales, has_prev ? p.tensor_scale[0] : 0.0f, has_prev,
+  mom_update_block(p.g, grad_scale, p.m, blk * 16, blk < p.nblk, p.codes, p.scales, has_prev ? p.tensor_scale[0] : 0.0f, has_prev,
                    p.prev_mask, p.mask, rotate, b1, b2, &sc[i], wg, status);
 }
 
@@ -1511,9 +1512,10 @@ __global__ __launch_bounds__(256) void k_root_mom_encode(RootChunk ch, int rotat
 }
 
 hipError_t launch_root_momentum(const RootChunk& ch, bool has_prev, bool rotate, bool adaptive, bool sr, float b1,
-                                float b2, MatScalars* sc, uint32_t* status, hipStream_t st) {
+                                float b2, const float* grad_scale, MatScalars* sc, uint32_t* status, hipStream_t st) {
   const dim3 grid(ch.end[ch.count - 1]);
-  hipLaunchKernelGGL(k_root_mom_update, grid, dim3(256), 0, st, ch, (int)has_prev, (int)rotate, b1, b2, sc, status);
+  hipLaunchKernelGGL(k_root_mom_update, grid, dim3(256), 0, st, ch, (int)has_prev, (int)rotate, b1, b2, grad_scale,
+                     sc, status);
   if (sr)
     hipLaunchKernelGGL(k_root_mom_encode<true>, grid, dim3(256), 0, st, ch, (int)rotate, (int)adaptive, sc);
   else
@@ -1527,7 +1529,7 @@ hipError_t launch_root_momentum(const RootChunk& ch, bool has_prev, bool rotate,
 // amax of m_t in slot 0 and saved the previous tensor scale in sg[kSlotPrevState]).
 // Each thread reads and writes only its own block of the state.
 template <bool SR>
-__global__ __launch_bounds__(256) void k_mom_encode(const float* g, uint8_t* codes, uint8_t* scales,
+__global__ __launch_bounds__(256) void k_mom_encode(const float* g, const float* grad_scale, uint8_t* codes, uint8_t* scales,
                                                     int64_t nblk, int has_prev, uint32_t prev_mask,
                                                     uint32_t mask, int rotate, int adaptive, float b1, float b2,
                                                     MatScalars* sc, float* tensor_scale, uint64_t sr_key) {
@@ -1546,6 +1548,7 @@ __global__ __launch_bounds__(256) void k_mom_encode(const float* g, uint8_t* cod
     const float4 v = gp[q];
     x[4 * q] = v.x; x[4 * q + 1] = v.y; x[4 * q + 2] = v.z; x[4 * q + 3] = v.w;
   }
+  scale16(x, grad_scale);
   float u[16];
   mom_block(x, codes, scales, e0, sc[0].sg[kSlotPrevState], has_prev != 0, prev_mask, rotate != 0, b1, b2, u);
   const float kf = rotate_for_quant(u, mask, rotate, sg);
@@ -1557,27 +1560,27 @@ __global__ __launch_bounds__(256) void k_mom_encode(const float* g, uint8_t* cod
   scales[blk] = (uint8_t)scale;
 }
 
-hipError_t launch_mom_encode(const float* g, uint8_t* codes, uint8_t* scales, int64_t n, bool has_prev,
+hipError_t launch_mom_encode(const float* g, const float* grad_scale, uint8_t* codes, uint8_t* scales, int64_t n, bool has_prev,
                              uint32_t prev_mask, uint32_t mask, bool rotate, bool adaptive, bool sr, float b1,
                              float b2, MatScalars* sc, float* tensor_scale, uint64_t sr_key, hipStream_t st) {
   const int64_t nblk = n / 16;
   const dim3 grid((uint32_t)((nblk + 255) / 256));
   if (sr)
-    hipLaunchKernelGGL(k_mom_encode<true>, grid, dim3(256), 0, st, g, codes, scales, nblk, (int)has_prev, prev_mask,
+    hipLaunchKernelGGL(k_mom_encode<true>, grid, dim3(256), 0, st, g, grad_scale, codes, scales, nblk, (int)has_prev, prev_mask,
                        mask, (int)rotate, (int)adaptive, b1, b2, sc, tensor_scale, sr_key);
   else
-    hipLaunchKernelGGL(k_mom_encode<false>, grid, dim3(256), 0, st, g, codes, scales, nblk, (int)has_prev, prev_mask,
+    hipLaunchKernelGGL(k_mom_encode<false>, grid, dim3(256), 0, st, g, grad_scale, codes, scales, nblk, (int)has_prev, prev_mask,
                        mask, (int)rotate, (int)adaptive, b1, b2, sc, tensor_scale, sr_key);
   return hipGetLastError();
 }
 
-hipError_t launch_mom_update(const float* g, float* m, int64_t batch, int64_t rows, int64_t cols,
+hipError_t launch_mom_update(const float* g, const float* grad_scale, float* m, int64_t batch, int64_t rows, int64_t cols,
                              const uint8_t* codes, const uint8_t* scales, const float* prev_sg,
                              bool has_prev, uint32_t prev_mask, uint32_t mask, bool rotate, float b1,
                              float b2, MatScalars* sc, uint32_t* status, hipStream_t st) {
   const int64_t nblk = rows * cols / 16;
   const dim3 grid((uint32_t)((nblk + 255) / 256), (uint32_t)batch);
-  hipLaunchKernelGGL(k_mom_update, grid, dim3(256), 0, st, g, m, rows, cols, codes, scales, prev_sg,
+  hipLaunchKernelGGL(k_mom_update, grid, dim3(256), 0, st, g, grad_scale, m, rows, cols, codes, scales, prev_sg,
                      (int)has_prev, prev_mask, mask, (int)rotate, b1, b2, sc, status);
   return hipGetLastError();
 }

@@ -1,0 +1,420 @@
+// Root-mean-square norm with the residual's addition and an output in E4M3, and its gradients.
+//   h = round_T(x + r),  rstd = 1 / sqrt(sum(h^2) / cols + eps),  y = (h rstd) gain
+//   per row, or per group of 32, 64 or 128 columns: amax = max(max |y|, 2^-100),
+//   s = amax / 448, or the smallest power of two with amax <= 448 s;  code = E4M3(y / s)
+// The squares are exact in binary64 and added there, so rstd is the rounding of the exact
+// value but for a few in 2^20 rows, and the scales and codes do not depend on how a row is
+// cut over threads.
+//   g = dy gain,  xhat = h rstd,  c = mean(g xhat),  dx = rstd (g - xhat c) + dh,
+//   dgain = sum over rows of dy xhat
+// Both passes are bound by memory: a row is read once and stays in registers.  A thread holds
+// vectors of 8 columns, TPR of them apart, so a group of columns lies in 4, 8 or 16 adjacent
+// lanes.  TPR threads share a row.
+#include "device.h"
+#include "internal.h"
+#include "vec.h"
+
+namespace fp4r {
+namespace {
+
+constexpr float kE4M3Max = 448.0f;
+constexpr float kAmaxMin = 0x1p-100f;
+
+// Lanes l and l ^ 1, l ^ 2 of a quad, then the other quad of 8 lanes, the other half of 16.
+template <int CTRL>
+FP4R_DEV float dpp_max(float v) {
+  return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true)));
+}
+FP4R_DEV float group_max(float v, int lanes) {   // lanes: 4, 8 or 16 (uniform)
+  v = dpp_max<0xB1>(v);
+  v = dpp_max<0x4E>(v);
+  if (lanes > 4) v = dpp_max<0x141>(v);
+  if (lanes > 8) v = dpp_max<0x140>(v);
+  return v;
+}
+
+FP4R_DEV double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+FP4R_DEV float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// 1 / sqrt(a) for 0 < a < 2^1000: the instruction's estimate and two Newton steps.
+FP4R_DEV double rsqrt64(double a) {
+  double r = __builtin_amdgcn_rsq(a);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const double e = __builtin_fma(-a * r, r, 1.0);
+    r = __builtin_fma(r * 0.5, e, r);
+  }
+  return r;
+}
+
+// The scale of a group as it is stored, and what its values are multiplied by.
+FP4R_DEV float scale_of(float amax, int e8m0, uint32_t& stored) {
+  amax = fmaxf(amax, kAmaxMin);
+  if (e8m0) {
+    // amax = 1.m 2^(e - 127) and 448 = 1.75 2^8
+    const uint32_t b = __float_as_uint(amax), e = (b >> 23) - 8u + ((b & 0x7FFFFFu) > 0x600000u);
+    stored = e;
+    return __uint_as_float((254u - e) << 23);
+  }
+  stored = __float_as_uint((float)((double)amax * (1.0 / 448.0)));
+  return (float)(448.0 * recip64(amax));
+}
+FP4R_DEV void store_scale(const RmsArgs& a, int64_t i, uint32_t stored) {
+  if (a.e8m0) reinterpret_cast<uint8_t*>(a.scales)[i] = (uint8_t)stored;
+  else reinterpret_cast<uint32_t*>(a.scales)[i] = stored;
+}
+
+FP4R_DEV void load_gain(const void* gain, int f32, int col, int n, float (&g)[8]) {
+  if (f32) unpack8(load_raw8((const float*)gain + col, n), g);
+  else unpack8(load_raw8((const bf16_t*)gain + col, n), g);
+}
+
+FP4R_DEV void store_codes(uint8_t* p, int n, const float (&y)[8], float inv) {
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k] * inv, y[4 * k + 1] * inv, 0, false);
+    w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2] * inv, y[4 * k + 3] * inv, v, true);
+  }
+  if (n >= 8) {
+    *reinterpret_cast<u32x2_a1*>(p) = u32x2{w[0], w[1]};
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) p[k] = (uint8_t)(w[k / 4] >> (8 * (k & 3)));
+  }
+}
+
+template <class T, int TPR, int VPT>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
+  constexpr int WPR = TPR / 64;                       // waves a row
+  constexpr int RPG = TPR < 256 ? 256 / TPR : 1;      // rows a workgroup
+  __shared__ double red_s[WPR];
+  __shared__ float red_m[WPR];
+  const int64_t row = (int64_t)blockIdx.x * RPG + threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR;
+  if (RPG > 1 && row >= a.rows) return;               // whole waves, and no barrier follows
+  Raw8<T> h[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    h[i] = load_raw8((const T*)a.x + row * a.ld_x + c, n);
+  }
+  if (a.r) {
+    Raw8<T> r[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+      r[i] = load_raw8((const T*)a.r + row * a.ld_r + c, n);
+    }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      float u[8], v[8];
+      unpack8(h[i], u);
+      unpack8(r[i], v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[k] += v[k];
+      h[i] = pack8<T>(u);
+    }
+  }
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    if (a.h) store_raw8((T*)a.h + row * a.ld_h + c, n, h[i]);
+    float u[8];
+    unpack8(h[i], u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s = __builtin_fma((double)u[k], (double)u[k], s);
+  }
+  s = wave_sum(s);
+  if constexpr (WPR > 1) {
+    if ((threadIdx.x & 63) == 0) red_s[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = red_s[0];
+#pragma unroll
+    for (int w = 1; w < WPR; ++w) s += red_s[w];
+  }
+  const float rstd = (float)rsqrt64(s / (double)a.cols + a.eps);
+  if (t == 0) {
+    if (a.rstd) a.rstd[row] = rstd;
+    if (a.status && !(s < __builtin_inf())) *a.status = kErrNonFinite;
+  }
+  if (!a.codes && !a.y) return;
+  float top = 0.0f;
+  const int lanes = a.group / 8;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    float y[8], g[8];
+    unpack8(h[i], y);
+    if (a.gain) {
+      load_gain(a.gain, a.gain_f32, c, n, g);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = (y[k] * rstd) * g[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] *= rstd;
+    }
+    if (a.y) store_raw8((T*)a.y + row * a.ld_y + c, n, pack8<T>(y));
+    if (!a.codes) continue;
+    float m = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf(y[k]));
+    if (lanes) {
+      m = group_max(m, lanes);
+      uint32_t stored;
+      const float inv = scale_of(m, a.e8m0, stored);
+      if (n > 0) store_codes(a.codes + row * a.cols + c, n, y, inv);
+      if (n > 0 && (t & (lanes - 1)) == 0) {
+        store_scale(a, row * a.groups + c / a.group, stored);
+        if (a.status && !(m < __builtin_inff())) *a.status = kErrNonFinite;
+      }
+    }
+    top = fmaxf(top, m);
+  }
+  if (!a.codes || lanes) return;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if constexpr (WPR > 1) {
+    if ((threadIdx.x & 63) == 0) red_m[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = red_m[0];
+#pragma unroll
+    for (int w = 1; w < WPR; ++w) top = fmaxf(top, red_m[w]);
+  }
+  uint32_t stored;
+  const float inv = scale_of(top, a.e8m0, stored);
+  if (t == 0) {
+    store_scale(a, row, stored);
+    if (a.status && !(top < __builtin_inff())) *a.status = kErrNonFinite;
+  }
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    if (n <= 0) continue;
+    float y[8], g[8];
+    unpack8(h[i], y);
+    if (a.gain) {
+      load_gain(a.gain, a.gain_f32, c, n, g);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = (y[k] * rstd) * g[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] *= rstd;
+    }
+    store_codes(a.codes + row * a.cols + c, n, y, inv);
+  }
+}
+
+template <class T, int TPR, int VPT>
+void run_rmsnorm(const RmsArgs& a, hipStream_t st) {
+  constexpr int NT = TPR < 256 ? 256 : TPR, RPG = NT / TPR;
+  hipLaunchKernelGGL((k_rmsnorm<T, TPR, VPT>), dim3((uint32_t)((a.rows + RPG - 1) / RPG)), dim3(NT), 0, st, a);
+}
+
+template <class T>
+void pick_rmsnorm(const RmsArgs& a, hipStream_t st) {
+  if (a.cols <= 512) run_rmsnorm<T, 64, 1>(a, st);
+  else if (a.cols <= 1024) run_rmsnorm<T, 64, 2>(a, st);
+  else if (a.cols <= 2048) run_rmsnorm<T, 256, 1>(a, st);
+  else if (a.cols <= 4096) run_rmsnorm<T, 256, 2>(a, st);
+  else if (a.cols <= 8192) run_rmsnorm<T, 256, 4>(a, st);
+  else if (a.cols <= 16384) run_rmsnorm<T, 1024, 2>(a, st);
+  else run_rmsnorm<T, 1024, 4>(a, st);
+}
+
+// ---------------------------------------------------------------------------
+// Gradients.  A workgroup of RPG row slots of TPR threads walks over rows, each thread keeping
+// its columns' part of dgain in registers; at the end the slots are added in LDS and the
+// workgroup writes one row of partials, which k_rms_dgain adds in order.
+
+template <class T, int TPR, int VPT>
+__global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_rms_bwd(RmsBwdArgs a) {
+  constexpr int NT = TPR < 512 ? 512 : TPR, RPG = NT / TPR, WPR = TPR / 64;
+  __shared__ float red[2][NT / 64];
+  __shared__ float slab[RPG > 1 ? NT * 8 : 1];
+  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  float acc[VPT][8];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[i][k] = 0.0f;
+  const float inv_cols = 1.0f / (float)a.cols;
+  int side = 0;
+  for (int64_t base = (int64_t)blockIdx.x * RPG; base < a.rows; base += (int64_t)gridDim.x * RPG, side ^= 1) {
+    const int64_t row = base + slot;
+    const bool live = row < a.rows;
+    Raw8<T> h[VPT], d[VPT], e[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int c = (i * TPR + t) * 8, n = live ? min(8, a.cols - c) : 0;
+      h[i] = load_raw8((const T*)a.h + row * a.ld_h + c, n);
+      d[i] = load_raw8((const T*)a.dy + row * a.ld_dy + c, n);
+    }
+    if (a.dh) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int c = (i * TPR + t) * 8, n = live ? min(8, a.cols - c) : 0;
+        e[i] = load_raw8((const T*)a.dh + row * a.ld_dh + c, n);
+      }
+    }
+    const float rstd = live ? a.rstd[row] : 0.0f;
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+      float x[8], y[8], g[8];
+      unpack8(h[i], x);
+      unpack8(d[i], y);
+      if (a.gain) {
+        load_gain(a.gain, a.gain_f32, c, n, g);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[k] = 1.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float xhat = x[k] * rstd;
+        acc[i][k] = fmaf(y[k], xhat, acc[i][k]);
+        dot = fmaf(y[k] * g[k], xhat, dot);
+      }
+    }
+    dot = wave_sum(dot);
+    if constexpr (WPR > 1) {
+      if ((threadIdx.x & 63) == 0) red[side][threadIdx.x >> 6] = dot;
+      __syncthreads();   // two sides: the next row's values do not overtake this row's readers
+      dot = red[side][slot * WPR];
+#pragma unroll
+      for (int w = 1; w < WPR; ++w) dot += red[side][slot * WPR + w];
+    }
+    const float mean = dot * inv_cols;
+    if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+      if (n <= 0) continue;
+      float x[8], y[8], g[8], o[8];
+      unpack8(h[i], x);
+      unpack8(d[i], y);
+      if (a.gain) {
+        load_gain(a.gain, a.gain_f32, c, n, g);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[k] = 1.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = rstd * (y[k] * g[k] - (x[k] * rstd) * mean);
+      if (a.dh) {
+        unpack8(e[i], x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] += x[k];
+      }
+      store_raw8((T*)a.dx + row * a.ld_dx + c, n, pack8<T>(o));
+    }
+  }
+  if (!a.dgain) return;
+  float* out = a.partial + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    if constexpr (RPG > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) slab[(slot * 8 + k) * TPR + t] = acc[i][k];
+      __syncthreads();
+      if (slot == 0) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          for (int q = 1; q < RPG; ++q) acc[i][k] += slab[(q * 8 + k) * TPR + t];
+      }
+    }
+    if (slot == 0 && n > 0) store_vec<float, 8>(out + c, n, acc[i]);
+  }
+}
+
+// 64 columns by 16 slices of the partial rows a workgroup.
+__global__ __launch_bounds__(1024) void k_rms_dgain(const float* partial, int64_t count, int cols, float* dgain) {
+  __shared__ float red[16][64];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+  float s = 0.0f;
+  if (c < cols)
+    for (int64_t p = slice; p < count; p += 16) s += partial[p * cols + c];
+  red[slice][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (slice == 0 && c < cols) {
+#pragma unroll
+    for (int q = 1; q < 16; ++q) s += red[q][threadIdx.x & 63];
+    dgain[c] = s;
+  }
+}
+
+struct BwdShape {
+  int tpr, vpt;
+};
+BwdShape bwd_shape(int64_t cols) {
+  const int tpr = cols <= 1024 ? 64 : cols <= 8192 ? 256 : 1024;
+  const int64_t v = (cols + 8 * tpr - 1) / (8 * tpr);
+  return {tpr, v <= 1 ? 1 : v <= 2 ? 2 : 4};
+}
+
+template <class T>
+void run_bwd(const RmsBwdArgs& a, uint32_t grid, hipStream_t st) {
+  const BwdShape s = bwd_shape(a.cols);
+  const dim3 nt(s.tpr < 512 ? 512 : s.tpr);
+#define FP4R_BWD(TPR, VPT)                                                              \
+  if (s.tpr == TPR && s.vpt == VPT) {                                                   \
+    hipLaunchKernelGGL((k_rms_bwd<T, TPR, VPT>), dim3(grid), nt, 0, st, a);             \
+    return;                                                                             \
+  }
+  FP4R_BWD(64, 1)
+  FP4R_BWD(64, 2)
+  FP4R_BWD(256, 1)
+  FP4R_BWD(256, 2)
+  FP4R_BWD(256, 4)
+  FP4R_BWD(1024, 2)
+  FP4R_BWD(1024, 4)
+#undef FP4R_BWD
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st) {
+  switch (a.type) {
+    case 0: pick_rmsnorm<float>(a, st); break;
+    case 1: pick_rmsnorm<bf16_t>(a, st); break;
+    default: pick_rmsnorm<f16_t>(a, st); break;
+  }
+  return hipGetLastError();
+}
+
+int64_t rms_bwd_groups(int64_t rows, int64_t cols) {
+  const int tpr = bwd_shape(cols).tpr, slots = tpr < 512 ? 512 / tpr : 1;
+  const int64_t all = (rows + slots - 1) / slots;
+  return all < 512 ? all : 512;
+}
+
+hipError_t launch_rmsnorm_backward(const RmsBwdArgs& a, hipStream_t st) {
+  const uint32_t grid = (uint32_t)rms_bwd_groups(a.rows, a.cols);
+  if (grid) {
+    switch (a.type) {
+      case 0: run_bwd<float>(a, grid, st); break;
+      case 1: run_bwd<bf16_t>(a, grid, st); break;
+      default: run_bwd<f16_t>(a, grid, st); break;
+    }
+  }
+  if (a.dgain)
+    hipLaunchKernelGGL(k_rms_dgain, dim3((uint32_t)((a.cols + 63) / 64)), dim3(1024), 0, st, a.partial, (int64_t)grid,
+                       (int)a.cols, a.dgain);
+  return hipGetLastError();
+}
+
+}  // namespace fp4r

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -57,6 +58,26 @@ class RootConfig(ctypes.Structure):
                 ("momentum_flags", ctypes.c_uint32), ("momentum_seed", ctypes.c_uint64), ("step", ctypes.c_int32)]
 
 
+FLOAT32, BFLOAT16, FLOAT16 = 0, 1, 2
+NORM_L2, NORM_MAX = 0, 1
+SCALE_FP32, SCALE_E8M0 = 0, 1
+_TYPES = {torch.float32: FLOAT32, torch.bfloat16: BFLOAT16, torch.float16: FLOAT16}
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld_in", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+                ("in_type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
+
+
+class RmsNorm(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in
+                ("x", "residual", "gain", "h", "y", "codes", "scales", "rstd", "status")] + \
+               [(name, ctypes.c_int64) for name in ("rows", "cols", "ld_x", "ld_residual", "ld_h", "ld_y")] + \
+               [(name, ctypes.c_int32) for name in ("type", "gain_type", "group", "scale_type")] + \
+               [("eps", ctypes.c_double)]
+
+
 class NsTrace(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in (
         "qx_codes", "qx_scales", "qx_sg", "qxt_codes", "qxt_scales", "qxt_sg", "A",
@@ -78,7 +99,7 @@ def load(path: str = None) -> ctypes.CDLL:
     lib = ctypes.CDLL(path)
     i64, u32, u64, f32, vp, i32 = (ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64,
                                    ctypes.c_float, ctypes.c_void_p, ctypes.c_int32)
-    sz = ctypes.c_size_t
+    sz, f64 = ctypes.c_size_t, ctypes.c_double
     lib.fp4root_quantize_workspace.argtypes = [i64, i64, i64, u32]
     lib.fp4root_quantize_workspace.restype = sz
     lib.fp4root_ns_step_workspace.argtypes = [i64, i64, i64, u32]
@@ -112,6 +133,30 @@ def load(path: str = None) -> ctypes.CDLL:
     lib.fp4root_root_step.argtypes = [ctypes.POINTER(Param), i64, ctypes.POINTER(RootConfig),
                                       ctypes.POINTER(NsConfig), vp, sz, vp]
     lib.fp4root_root_step.restype = ctypes.c_int
+    lib.fp4root_grad_norm_workspace.argtypes = [ctypes.POINTER(Tensor), i64]
+    lib.fp4root_grad_norm_workspace.restype = sz
+    lib.fp4root_grad_norm.argtypes = [ctypes.POINTER(Tensor), i64, ctypes.c_int, f64, f64, vp, vp, vp, vp, sz, vp]
+    lib.fp4root_grad_norm.restype = ctypes.c_int
+    lib.fp4root_clip_coef.argtypes = [vp, ctypes.c_int, f64, f64, vp, vp]
+    lib.fp4root_clip_coef.restype = ctypes.c_int
+    lib.fp4root_clip_grads.argtypes = [ctypes.POINTER(Tensor), i64, vp, vp]
+    lib.fp4root_clip_grads.restype = ctypes.c_int
+    lib.fp4root_momentum_update_scaled.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp, f32, u32, u64, i32, vp, vp, sz,
+                                                   vp]
+    lib.fp4root_momentum_update_scaled.restype = ctypes.c_int
+    lib.fp4root_qadamw_update_scaled.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, f32, f32, f32, f32, f32,
+                                                 u32, u64, i32, vp, vp, sz, vp]
+    lib.fp4root_qadamw_update_scaled.restype = ctypes.c_int
+    lib.fp4root_root_step_scaled.argtypes = [ctypes.POINTER(Param), i64, ctypes.POINTER(RootConfig),
+                                             ctypes.POINTER(NsConfig), vp, vp, sz, vp]
+    lib.fp4root_root_step_scaled.restype = ctypes.c_int
+    lib.fp4root_rmsnorm_quantize.argtypes = [ctypes.POINTER(RmsNorm), vp]
+    lib.fp4root_rmsnorm_quantize.restype = ctypes.c_int
+    lib.fp4root_rmsnorm_backward_workspace.argtypes = [i64, i64]
+    lib.fp4root_rmsnorm_backward_workspace.restype = sz
+    lib.fp4root_rmsnorm_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, i64, ctypes.c_int,
+                                             ctypes.c_int, vp, sz, vp]
+    lib.fp4root_rmsnorm_backward.restype = ctypes.c_int
     lib.fp4root_default_coeffs.argtypes = [i64, i64, i32, ctypes.POINTER(ctypes.c_float)]
     lib.fp4root_default_coeffs.restype = ctypes.c_int
     lib.fp4root_device_status.argtypes = [vp, vp]
@@ -162,6 +207,15 @@ def _need_gpu_f32(x: torch.Tensor, name: str):
         raise TypeError(f"{name} must be a GPU tensor")
     if x.dtype != torch.float32:
         raise TypeError(f"{name} must be float32")
+
+
+def _grad_scale(t, device):
+    if t is None:
+        return None
+    _need_gpu_f32(t, "grad_scale")
+    if t.numel() != 1 or t.device != device:
+        raise ValueError("grad_scale must be one element on the gradients' GPU")
+    return _ptr(t)
 
 
 def workspace(nbytes: int, device) -> torch.Tensor:
@@ -315,9 +369,10 @@ class MomentumState:
 
 def fp4root_momentum_update(g: torch.Tensor, state: MomentumState, beta: float, step: int,
                             flags: int = F_HADAMARD | F_ADAPTIVE46 | F_STOCHASTIC, seed: int = 0,
-                            m: torch.Tensor = None, stream=None) -> torch.Tensor:
+                            m: torch.Tensor = None, stream=None, grad_scale: torch.Tensor = None) -> torch.Tensor:
     """One first-moment step: returns m_t (FP32, shape of g) and re-encodes `state`.
-    g: (rows, cols) or (B, rows, cols) contiguous float32.  See include/fp4root.h."""
+    g: (rows, cols) or (B, rows, cols) contiguous float32; grad_scale: a float32 GPU
+    tensor of one element that multiplies g (GradClipper.coef).  See include/fp4root.h."""
     _need_gpu_f32(g, "g")
     if not g.is_contiguous():
         raise ValueError("g must be contiguous")
@@ -330,9 +385,10 @@ def fp4root_momentum_update(g: torch.Tensor, state: MomentumState, beta: float, 
     _need_gpu_f32(m, "m")
     if m.shape != g.shape or not m.is_contiguous():
         raise ValueError("m must be a contiguous tensor of g's shape")
-    _check(load().fp4root_momentum_update(_ptr(gb), _ptr(m), B, R, C, _ptr(state.codes), _ptr(state.scales),
-                                          _ptr(state.tensor_scale), beta, flags, seed, step, _ptr(state.ws),
-                                          state.ws.numel(), _stream(stream)), "fp4root_momentum_update")
+    _check(load().fp4root_momentum_update_scaled(
+        _ptr(gb), _ptr(m), B, R, C, _ptr(state.codes), _ptr(state.scales), _ptr(state.tensor_scale), beta, flags, seed,
+        step, _grad_scale(grad_scale, g.device), _ptr(state.ws), state.ws.numel(), _stream(stream)),
+        "fp4root_momentum_update")
     return m
 
 
@@ -367,31 +423,36 @@ class QAdamWState:
 
 def fp4root_qadamw_update(w: torch.Tensor, g: torch.Tensor, state: QAdamWState, step: int, lr: float,
                           wd: float = 0.1, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
-                          flags: int = F_HADAMARD | F_ADAPTIVE46 | F_STOCHASTIC, seed: int = 0, stream=None):
-    """One quantized-state AdamW step on a flat contiguous bfloat16 parameter w with FP32 gradient g."""
+                          flags: int = F_HADAMARD | F_ADAPTIVE46 | F_STOCHASTIC, seed: int = 0, stream=None,
+                          grad_scale: torch.Tensor = None):
+    """One quantized-state AdamW step on a flat contiguous bfloat16 parameter w with FP32 gradient g
+    (times grad_scale, a float32 GPU tensor of one element, if given)."""
     if w.dtype != torch.bfloat16 or not w.is_cuda or not w.is_contiguous():
         raise TypeError("w must be a contiguous bfloat16 GPU tensor")
     _need_gpu_f32(g, "g")
     if g.numel() != w.numel() or not g.is_contiguous() or w.numel() != state.n:
         raise ValueError("g and state must match w")
-    _check(load().fp4root_qadamw_update(
+    _check(load().fp4root_qadamw_update_scaled(
         _ptr(w), _ptr(g), _ptr(state.m), state.n, _ptr(state.m_codes), _ptr(state.m_scales),
         _ptr(state.m_tensor_scale), _ptr(state.v_codes), _ptr(state.v_scales), _ptr(state.v_means),
-        lr, wd, beta1, beta2, eps, flags, seed, step, _ptr(state.ws), state.ws.numel(), _stream(stream)),
-        "fp4root_qadamw_update")
+        lr, wd, beta1, beta2, eps, flags, seed, step, _grad_scale(grad_scale, w.device), _ptr(state.ws),
+        state.ws.numel(), _stream(stream)), "fp4root_qadamw_update")
 
 
 class RootStep:
     """Reusable fp4root_root_step over a fixed list of (BF16 weight, FP32 gradient) pairs.
 
     Holds the descriptors, each parameter's first-moment state and FP32 scratch,
-    the configurations and the workspace; each call is one C call.
+    the configurations and the workspace; each call is one C call.  With max_norm every call
+    first takes the gradients' global norm (self.clipper, a GradClipper) and the step reads
+    them times its clipping coefficient; a norm over more tensors than these is taken by a
+    GradClipper of the caller's, whose coef goes into the call as grad_scale.
     """
 
     def __init__(self, weights, grads, lr: float, wd: float = 0.1, beta: float = 0.9, steps: int = 5,
                  coeffs=None, ns_flags: int = F_DEFAULT, momentum_flags: int = F_HADAMARD | F_ADAPTIVE46 | F_STOCHASTIC,
                  clip_quantile: float = 0.99, eps: float = 1e-7, seed: int = 0, momentum_seed: int = 0,
-                 scales=None):
+                 scales=None, max_norm: float = None):
         lib = load()
         self.weights, self.grads = list(weights), list(grads)
         n = len(self.weights)
@@ -426,14 +487,346 @@ class RootStep:
         if need == 0:
             raise ValueError("invalid parameters or configuration")
         self.ws = workspace(need, self.weights[0].device if n else torch.device("cuda"))
+        self.clipper = GradClipper(self.grads, max_norm) if max_norm is not None and n else None
 
-    def __call__(self, step: int, stream=None):
+    def __call__(self, step: int, stream=None, grad_scale: torch.Tensor = None):
         self.cfg.step = step
-        _check(load().fp4root_root_step(self.params, self.count, ctypes.byref(self.cfg), ctypes.byref(self.ns),
-                                        _ptr(self.ws), self.ws.numel(), _stream(stream)), "fp4root_root_step")
+        if self.clipper is not None:
+            if grad_scale is not None:
+                raise ValueError("max_norm and grad_scale exclude each other")
+            self.clipper.norm(stream)
+            grad_scale = self.clipper.coef
+        scale = _grad_scale(grad_scale, self.ws.device)
+        _check(load().fp4root_root_step_scaled(self.params, self.count, ctypes.byref(self.cfg), ctypes.byref(self.ns),
+                                               scale, _ptr(self.ws), self.ws.numel(), _stream(stream)),
+               "fp4root_root_step")
 
     def status(self, stream=None) -> int:
         return fp4root_device_status(self.ws, stream)
+
+
+def _launch_stream(device, stream):
+    """The stream of a call on tensors of `device`: the given one, or the current one there."""
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    if stream.device != device:
+        raise ValueError("the stream belongs to another GPU than the tensors")
+    return stream
+
+
+def _call(fn, device, *args):
+    """fn(*args) with `device` current: kernels are launched on the current GPU's code."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return fn(*args)
+    return fn(*args)
+
+
+def _as_rows(t: torch.Tensor, name: str):
+    """(rows, cols, row stride) under which a kernel walks t in the order of its memory."""
+    if t.numel() == 0:
+        return 0, 0, 0
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    order = sorted((i for i in range(t.dim()) if t.shape[i] > 1), key=lambda i: (t.stride(i), t.shape[i]))
+    sizes = [(t.shape[i], t.stride(i)) for i in order]
+    if sizes[0][1] != 1:
+        sizes.insert(0, (1, 1))
+    cols, k = sizes[0][0], 1
+    while k < len(sizes) and sizes[k][1] == cols:      # the innermost run of memory
+        cols *= sizes[k][0]
+        k += 1
+    rows, ld = 1, sizes[k][1] if k < len(sizes) else cols
+    while k < len(sizes) and sizes[k][1] == rows * ld:
+        rows *= sizes[k][0]
+        k += 1
+    if k < len(sizes) or (rows > 1 and ld < cols):
+        raise ValueError(f"{name} must be rows of one stride (contiguous, a slice of columns, or a transpose of these)")
+    return rows, cols, ld
+
+
+class GradClipper:
+    """The global norm of a fixed list of gradient tensors (float32, bfloat16 or float16, mixed
+    as they come) and the clipping by it; see fp4root_grad_norm and fp4root_clip_grads in
+    include/fp4root.h.  Holds the descriptors, the workspace and the results:
+
+      total       float64 [1]: the sum of squares (norm_type 2) or largest magnitude (inf)
+      norms       float32 [len(grads)]: each tensor's norm
+      total_norm  float32 scalar, coef float32 scalar: min(1, max_norm / (total_norm + eps))
+
+    `norm()` computes these; a call computes them and multiplies every gradient by coef, into
+    `outputs` (tensors of the gradients' shapes and any of the types, or None: in place).  Ranks
+    that hold shards run `norm()`, all-reduce `total` (sum, or maximum for inf), then `recoef()`
+    and `scale()`.  RootStep, fp4root_qadamw_update and fp4root_momentum_update take `coef` as
+    grad_scale and then need no scaled gradients.  Each may be captured into a HIP graph; calls
+    of one GradClipper on two streams at once race.  Gradients must stay where they are.
+    """
+
+    def __init__(self, grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6):
+        lib = load()
+        self.grads = list(grads)
+        self.outputs = list(outputs) if outputs is not None else self.grads
+        if len(self.outputs) != len(self.grads):
+            raise ValueError("outputs must match grads")
+        if norm_type not in (2, float("inf")):
+            raise ValueError("norm_type must be 2 or inf")
+        if not max_norm > 0 or not 0 <= eps < float("inf"):
+            raise ValueError("max_norm must be positive and eps non-negative")
+        self.kind = NORM_L2 if norm_type == 2 else NORM_MAX
+        self.max_norm, self.eps = float(max_norm), float(eps)
+        n = len(self.grads)
+        self.tensors = (Tensor * max(n, 1))()
+        self.device = self.grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        for i, (g, o) in enumerate(zip(self.grads, self.outputs)):
+            for name, t in ((f"grads[{i}]", g), (f"outputs[{i}]", o)):
+                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != self.device:
+                    raise TypeError(f"{name} must be a tensor on the first gradient's GPU")
+                if t.dtype not in _TYPES:
+                    raise TypeError(f"{name} must be float32, bfloat16 or float16")
+            rows, cols, ld = _as_rows(g, f"grads[{i}]")
+            ld_out = ld
+            if o is not g:
+                if o.shape != g.shape:
+                    raise ValueError(f"outputs[{i}] must have the gradient's shape")
+                ri, ci, ld_out = _as_rows(o, f"outputs[{i}]")
+                order = [[t.stride(d) for d in range(t.dim()) if t.shape[d] > 1] for t in (g, o)]
+                if sorted(range(len(order[0])), key=order[0].__getitem__) != \
+                        sorted(range(len(order[1])), key=order[1].__getitem__):
+                    raise ValueError(f"outputs[{i}] must have its dimensions in memory in the gradient's order")
+                # a contiguous one beside one of rows is taken as those rows
+                if (ri, ci) != (rows, cols):
+                    if ri == 1 and rows * cols == ci:
+                        ld_out = cols
+                    elif rows == 1 and ri * ci == cols:
+                        rows, cols, ld = ri, ci, ci
+                    else:
+                        raise ValueError(f"outputs[{i}] must be laid out as the gradient, or contiguous")
+            self.tensors[i] = Tensor(g.data_ptr(), o.data_ptr(), rows, cols, ld, ld_out, _TYPES[g.dtype],
+                                     _TYPES[o.dtype])
+        self.count = n
+        need = lib.fp4root_grad_norm_workspace(self.tensors, n)
+        if need == 0:
+            raise ValueError("invalid gradients")
+        self.ws = workspace(need, self.device)
+        self.total = torch.zeros(1, dtype=torch.float64, device=self.device)
+        self.norms = torch.zeros(n, dtype=torch.float32, device=self.device)
+        self.result = torch.zeros(2, dtype=torch.float32, device=self.device)
+        self.total_norm, self.coef = self.result[0], self.result[1]
+        self._args = (_ptr(self.total), _ptr(self.norms) if n else None, _ptr(self.result), _ptr(self.ws),
+                      self.ws.numel())
+        self._coef = _ptr(self.coef)
+
+    def norm(self, stream=None) -> torch.Tensor:
+        """The norm (self.total_norm), and with it total, norms and coef."""
+        s = _launch_stream(self.device, stream).cuda_stream
+        _check(_call(load().fp4root_grad_norm, self.device, self.tensors, self.count, self.kind, self.max_norm,
+                     self.eps, *self._args, s), "fp4root_grad_norm")
+        return self.total_norm
+
+    def recoef(self, stream=None) -> torch.Tensor:
+        """total_norm and coef again, from `total` (after an all-reduce)."""
+        s = _launch_stream(self.device, stream).cuda_stream
+        _check(_call(load().fp4root_clip_coef, self.device, self._args[0], self.kind, self.max_norm, self.eps,
+                     self._args[2], s), "fp4root_clip_coef")
+        return self.total_norm
+
+    def scale(self, stream=None):
+        """Every gradient times coef, into the outputs, which it returns."""
+        s = _launch_stream(self.device, stream).cuda_stream
+        _check(_call(load().fp4root_clip_grads, self.device, self.tensors, self.count, self._coef, s),
+               "fp4root_clip_grads")
+        return self.outputs
+
+    def __call__(self, stream=None):
+        self.norm(stream)
+        return self.scale(stream)
+
+    def status(self, stream=None) -> int:
+        """FP4ROOT_ERR_NONFINITE where the last norm met a NaN or an infinity, else 0 (waits)."""
+        return fp4root_device_status(self.ws, _launch_stream(self.device, stream))
+
+
+def fp4root_clip_grads(grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6, stream=None):
+    """Clip a list of gradient tensors by their global norm, in place or into `outputs`; returns
+    the norm before clipping (a float32 GPU scalar).  A program that clips the same buffers step
+    after step keeps a GradClipper instead."""
+    c = GradClipper(grads, max_norm, outputs, norm_type, eps)
+    c(stream)
+    if stream is not None:                 # the results were allocated on the current stream
+        for t in (c.ws, c.total, c.norms, c.result):
+            t.record_stream(stream)
+    return c.total_norm
+
+
+class RmsNormOutput(NamedTuple):
+    """codes: uint8 E4M3FN codes of the input's shape; scales: float32, or uint8 exponents
+    (E8M0); rstd: float32 per row; h: the stream after the residual's addition (x itself
+    without a residual); y: the unquantized output if wanted."""
+    codes: Optional[torch.Tensor]
+    scales: Optional[torch.Tensor]
+    rstd: torch.Tensor
+    h: torch.Tensor
+    y: Optional[torch.Tensor]
+
+
+def _matrix(t: torch.Tensor, name: str, like: torch.Tensor = None):
+    """(rows, row stride) of a tensor whose last dimension is contiguous and whose others are
+    rows of one stride; checked against `like` for type, shape and GPU."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if like is not None and (t.dtype != like.dtype or t.shape != like.shape or t.device != like.device):
+        raise TypeError(f"{name} must have x's type, shape and GPU")
+    if t.is_contiguous():
+        cols = t.shape[-1]
+        return (t.numel() // cols if cols else 0), cols
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} rows must be contiguous")
+    lead = [(t.shape[i], t.stride(i)) for i in range(t.dim() - 1) if t.shape[i] > 1]
+    rows, ld = 1, t.shape[-1]
+    for k, (n, s) in enumerate(reversed(lead)):
+        if k == 0:
+            ld = s
+        elif s != rows * ld:
+            raise ValueError(f"{name} must be rows of one stride")
+        rows *= n
+    if rows > 1 and ld < t.shape[-1]:
+        raise ValueError(f"{name} rows must not overlap")
+    return (0 if t.numel() == 0 else rows), ld
+
+
+def _gain_type(gain, x):
+    if gain is None:
+        return FLOAT32
+    if not isinstance(gain, torch.Tensor) or not gain.is_cuda or gain.device != x.device or \
+            gain.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("gain must be a float32 or bfloat16 tensor on x's GPU")
+    if gain.dim() != 1 or gain.shape[0] != x.shape[-1] or not gain.is_contiguous():
+        raise ValueError("gain must be a contiguous vector of x's columns")
+    return _TYPES[gain.dtype]
+
+
+def _need_stream(x, name: str):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if x.dtype not in _TYPES:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16")
+    if x.dim() < 1:
+        raise ValueError(f"{name} must have a dimension of columns")
+
+
+def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residual: torch.Tensor = None,
+                             eps: float = 1e-6, group: int = 0, e8m0: bool = False, quantize: bool = True,
+                             want_y: bool = False, out: RmsNormOutput = None, status: torch.Tensor = None,
+                             stream=None) -> RmsNormOutput:
+    """h = x + residual, then its root-mean-square norm times gain, in E4M3 with a scale per row
+    (group 0) or per group of 32, 64 or 128 columns.  x: (..., cols), float32, bfloat16 or
+    float16, rows of one stride; out: an earlier call's result, whose tensors are written again
+    (h may be the residual or x itself: in place); status: an int32 GPU tensor of one element.
+    See fp4root_rmsnorm_quantize in include/fp4root.h."""
+    _need_stream(x, "x")
+    a = RmsNorm()
+    a.type, a.gain_type = _TYPES[x.dtype], _gain_type(gain, x)
+    a.rows, a.ld_x = _matrix(x, "x")
+    cols = a.cols = x.shape[-1]
+    dev = x.device
+    a.x = x.data_ptr()
+    if gain is not None:
+        a.gain = gain.data_ptr()
+    if residual is not None:
+        a.ld_residual = _matrix(residual, "residual", x)[1]
+        a.residual = residual.data_ptr()
+    a.group, a.scale_type, a.eps = group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps
+    lead = x.shape[:-1]
+    stream_ = _launch_stream(dev, stream)
+    if out is None:
+        codes = scales = y = None
+        if quantize:
+            codes = torch.empty(x.shape, dtype=torch.uint8, device=dev)
+            shape = (*lead, -(-cols // group)) if group > 0 else lead
+            scales = torch.empty(shape, dtype=torch.uint8 if e8m0 else torch.float32, device=dev)
+        rstd = torch.empty(lead, dtype=torch.float32, device=dev)
+        h = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device=dev)
+        if want_y:
+            y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        out = RmsNormOutput(codes, scales, rstd, h, y)
+        if stream is not None:
+            for t in out:
+                if t is not None and t is not x:
+                    t.record_stream(stream)
+    else:
+        codes, scales, rstd, h, y = out
+        for name, t, dtype, shape in (("codes", codes, torch.uint8, x.shape),
+                                      ("scales", scales, torch.uint8 if e8m0 else torch.float32,
+                                       (*lead, -(-cols // group)) if group > 0 else tuple(lead)),
+                                      ("rstd", rstd, torch.float32, lead)):
+            if t is None:
+                continue
+            if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"out.{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on x's GPU")
+    if residual is None:
+        out = out._replace(h=x)            # the stream is x: nothing to write
+    elif h is not None:
+        a.ld_h = _matrix(h, "out.h", x)[1]
+        a.h = h.data_ptr()
+    if y is not None:
+        a.ld_y = _matrix(y, "out.y", x)[1]
+        a.y = y.data_ptr()
+    if codes is not None:
+        a.codes = codes.data_ptr()
+    if scales is not None:
+        a.scales = scales.data_ptr()
+    if rstd is not None:
+        a.rstd = rstd.data_ptr()
+    if status is not None:
+        if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
+            raise ValueError("status must be one int32 element on x's GPU")
+        a.status = status.data_ptr()
+    _check(_call(load().fp4root_rmsnorm_quantize, dev, ctypes.byref(a), stream_.cuda_stream),
+           "fp4root_rmsnorm_quantize")
+    return out
+
+
+def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[torch.Tensor], rstd: torch.Tensor,
+                             dh: torch.Tensor = None, dx: torch.Tensor = None, dgain: torch.Tensor = None,
+                             want_dgain: bool = True, ws: torch.Tensor = None, stream=None):
+    """(dx, dgain) of the norm of h under the gradient dy of its output and dh of h itself; dx in
+    h's type is the gradient of x and of the residual alike, dgain is float32.  dx may be given
+    (dy, h or dh itself: in place); see fp4root_rmsnorm_backward in include/fp4root.h."""
+    _need_stream(h, "h")
+    rows, ld_h = _matrix(h, "h")
+    ld_dy = _matrix(dy, "dy", h)[1]
+    ld_dh = _matrix(dh, "dh", h)[1] if dh is not None else 0
+    cols, dev = h.shape[-1], h.device
+    gain_type = _gain_type(gain, h)
+    _need_gpu_f32(rstd, "rstd")
+    if rstd.numel() != rows or not rstd.is_contiguous() or rstd.device != dev:
+        raise ValueError("rstd must hold one contiguous element per row on h's GPU")
+    stream_ = _launch_stream(dev, stream)
+    new = []
+    if dx is None:
+        dx = torch.empty(h.shape, dtype=h.dtype, device=dev)
+        new.append(dx)
+    ld_dx = _matrix(dx, "dx", h)[1]
+    need = 0
+    if dgain is None and want_dgain:
+        dgain = torch.empty(cols, dtype=torch.float32, device=dev)
+        new.append(dgain)
+    if dgain is not None:
+        _need_gpu_f32(dgain, "dgain")
+        if dgain.numel() != cols or not dgain.is_contiguous() or dgain.device != dev:
+            raise ValueError("dgain must hold one contiguous element per column on h's GPU")
+        need = load().fp4root_rmsnorm_backward_workspace(rows, cols)
+        if ws is None or ws.numel() < need:
+            ws = workspace(need, dev)
+            new.append(ws)
+    if stream is not None:
+        for t in new:
+            t.record_stream(stream)
+    _check(_call(load().fp4root_rmsnorm_backward, dev, _ptr(dy), ld_dy, _ptr(h), ld_h, _ptr(dh), ld_dh, _ptr(gain),
+                 _ptr(rstd), _ptr(dx), ld_dx, _ptr(dgain), rows, cols, _TYPES[h.dtype], gain_type,
+                 _ptr(ws) if need else None, ws.numel() if need else 0, stream_.cuda_stream),
+           "fp4root_rmsnorm_backward")
+    return dx, dgain
 
 
 class Orthogonalizer:
