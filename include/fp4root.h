@@ -336,7 +336,8 @@ enum {
 /* One tensor of a gradient list: rows x cols elements of type in_type at `in` (device, at
  * the element's alignment), row stride ld_in >= cols; a contiguous tensor of any shape may be
  * given as one row.  rows or cols may be 0 (then the pointers may be NULL).  out, ld_out and
- * out_type: where fp4root_clip_grads writes; fp4root_grad_norm does not read them. */
+ * out_type: where fp4root_clip_grads writes; out may be `in` itself, with the same type and
+ * stride, and NULL in every tensor of a list that is only measured. */
 typedef struct {
   const void* in;
   void* out;
@@ -344,10 +345,26 @@ typedef struct {
   int32_t in_type, out_type;
 } fp4root_tensor;
 
-/* Workspace bytes fp4root_grad_norm needs for this list, or 0 for an invalid one. */
-size_t fp4root_grad_norm_workspace(const fp4root_tensor* tensors, int64_t count);
+/* A list of gradient tensors that stay where they are from step to step (host memory, written
+ * by fp4root_grad_list_init, and not to be changed).  The device memory behind it holds a table
+ * of the tensors and the scratch of the norm; it starts with the list's status word. */
+typedef struct {
+  void* mem;
+  int64_t count, parts;
+  int32_t outputs;   /* whether the tensors have outputs */
+} fp4root_grad_list;
 
-/* The norm of all elements of `count` tensors (host array, at most 2^20) taken together.
+/* Device bytes of a list of `count` tensors (host array, at most 2^20), or 0 for an invalid one. */
+size_t fp4root_grad_list_size(const fp4root_tensor* tensors, int64_t count);
+
+/* Writes the table into `mem` (mem_bytes >= the size above, 256-byte aligned) and the handle
+ * into *list.  Asynchronous: calls on another stream have to wait for it.  An output that is
+ * not its own input but meets it or another tensor of the list, and a tensor written twice, are
+ * refused (FP4ROOT_ERR_INVALID_ARG). */
+int fp4root_grad_list_init(fp4root_grad_list* list, const fp4root_tensor* tensors, int64_t count, void* mem,
+                           size_t mem_bytes, void* stream);
+
+/* The norm of all elements of the list taken together.
  *   kind:   FP4ROOT_NORM_*; max_norm: > 0 (+inf: no clipping); eps: >= 0, finite;
  *   total:  device double, the sum of squares or the largest magnitude: what ranks that hold
  *           shards of the gradients add (or take the maximum of) before fp4root_clip_coef;
@@ -358,19 +375,18 @@ size_t fp4root_grad_norm_workspace(const fp4root_tensor* tensors, int64_t count)
  * size alone, so nothing overflows, a tensor's norm does not change with the tensors beside it
  * and repeated calls give the same bits.  A NaN makes the norms it enters and the coefficient
  * NaN; an infinity makes the norms infinite and the coefficient 0 (NaN where max_norm is
- * infinite too); both are reported by fp4root_device_status(ws). */
-int fp4root_grad_norm(const fp4root_tensor* tensors, int64_t count, int kind, double max_norm, double eps,
-                      double* total, float* norms, float* result, void* ws, size_t ws_bytes, void* stream);
+ * infinite too); both are reported by fp4root_device_status(list->mem).  Calls on one list that
+ * overlap in time race. */
+int fp4root_grad_norm(const fp4root_grad_list* list, int kind, double max_norm, double eps, double* total,
+                      float* norms, float* result, void* stream);
 
 /* result (as above) from a total on the device. */
 int fp4root_clip_coef(const double* total, int kind, double max_norm, double eps, float* result, void* stream);
 
-/* out = round(fl32(in * *coef)) for every tensor of the list, coef a device float (result + 1
- * above).  out may be in itself, with the same type and stride (tensors that the coefficient 1
- * leaves as they are, are then not touched); any other overlap of an output with another
- * tensor of the list, or one tensor written twice, is refused.  A result past the output
- * type's largest becomes an infinity.  count is at most 2^20. */
-int fp4root_clip_grads(const fp4root_tensor* tensors, int64_t count, const float* coef, void* stream);
+/* out = round(fl32(in * *coef)) for every tensor of a list with outputs, coef a device float
+ * (result + 1 above).  Tensors in place that the coefficient 1 leaves as they are, are not
+ * touched.  A result past the output type's largest becomes an infinity. */
+int fp4root_clip_grads(const fp4root_grad_list* list, const float* coef, void* stream);
 
 /* fp4root_momentum_update, fp4root_qadamw_update and fp4root_root_step with every gradient
  * element g replaced by fl32(g * *grad_scale), grad_scale a device float: clipping without

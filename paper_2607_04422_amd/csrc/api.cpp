@@ -1410,7 +1410,6 @@ Span span(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
 }
 
 int check_tensors(const fp4root_tensor* t, int64_t count, bool out) {
-  if (count < 0 || count > kMaxTensors || (count > 0 && !t)) return FP4ROOT_ERR_INVALID_ARG;
   for (int64_t i = 0; i < count; ++i) {
     if (!type_ok(t[i].in_type) || (out && !type_ok(t[i].out_type))) return FP4ROOT_ERR_INVALID_ARG;
     if (t[i].rows < 0 || t[i].cols < 0) return FP4ROOT_ERR_SHAPE;
@@ -1463,8 +1462,8 @@ bool outputs_apart(const fp4root_tensor* t, int64_t count) {
 
 // The tensor as the kernels walk it: contiguous ones as a row, cut into parts of 2^shift
 // vectors, 64 KB at least, and into at most 1024 of them.
-int64_t grad_ref(const fp4root_tensor& t, bool out, GradRef& r, uint8_t& shift) {
-  r = GradRef{t.in, out ? t.out : nullptr, t.rows, t.cols, t.ld_in, out ? t.ld_out : 0, 0};
+GradRef grad_ref(const fp4root_tensor& t, bool out, int64_t& parts) {
+  GradRef r{t.in, out ? t.out : nullptr, t.rows, t.cols, t.ld_in, out ? t.ld_out : 0, 0, 0, 0, 0};
   if (t.rows == 0 || t.cols == 0) {
     r.rows = 1;
     r.cols = 0;
@@ -1476,48 +1475,45 @@ int64_t grad_ref(const fp4root_tensor& t, bool out, GradRef& r, uint8_t& shift) 
   r.vectors = r.rows * ((r.cols + ve - 1) / ve);
   int s = 12;
   while (r.vectors > int64_t(1024) << s) ++s;
-  shift = (uint8_t)s;
-  return std::max<int64_t>(1, (r.vectors + (int64_t(1) << s) - 1) >> s);
+  r.shift = (uint16_t)s;
+  r.type = (uint16_t)(t.in_type | (out ? t.out_type : 0) << 2);
+  parts = std::max<int64_t>(1, (r.vectors + (int64_t(1) << s) - 1) >> s);   // an empty tensor has one too
+  return r;
 }
 
-// Calls launch(chunk, first part, first tensor) for runs of up to kMaxGradChunk tensors.
-template <class F>
-int each_grad_chunk(const fp4root_tensor* t, int64_t count, bool out, F launch) {
-  int64_t part = 0;
-  for (int64_t i0 = 0; i0 < count; i0 += kMaxGradChunk) {
-    GradChunk ch;
-    ch.count = (int)std::min<int64_t>(kMaxGradChunk, count - i0);
-    int64_t end = 0;
-    for (int k = 0; k < ch.count; ++k) {
-      const fp4root_tensor& g = t[i0 + k];
-      end += grad_ref(g, out, ch.t[k], ch.shift[k]);
-      ch.end[k] = (uint32_t)end;
-      ch.type[k] = (uint8_t)(g.in_type | (out ? g.out_type : 0) << 2);
-    }
-    FP4R_TRY(launch(ch, (uint32_t)part, (uint32_t)i0));
-    part += end;
-  }
-  return FP4ROOT_OK;
-}
-
-int64_t grad_parts(const fp4root_tensor* t, int64_t count) {
-  int64_t parts = 0;
+// count is checked: 0 .. kMaxTensors
+bool has_outputs(const fp4root_tensor* t, int64_t count) {
+  bool empty = true;   // with no element at all there is nothing to write, and any call may do so
   for (int64_t i = 0; i < count; ++i) {
-    GradRef r;
-    uint8_t shift;
-    parts += grad_ref(t[i], false, r, shift);
+    if (t[i].out) return true;
+    empty = empty && (t[i].rows == 0 || t[i].cols == 0);
   }
-  return parts;
+  return empty;
 }
 
-size_t carve_grad_norm(void* base, int64_t count, int64_t parts, GradNormWs& w) {
+int64_t grad_parts(const fp4root_tensor* t, int64_t count, bool out) {
+  int64_t all = 0, parts;
+  for (int64_t i = 0; i < count; ++i) {
+    grad_ref(t[i], out, parts);
+    all += parts;
+  }
+  return all;
+}
+
+size_t carve_grad_list(void* base, int64_t count, int64_t parts, GradTable& w) {
   Carver cv(base);
   w.status = cv.take<uint32_t>(1);
   w.ticket = cv.take<uint32_t>(1);
-  w.first = cv.take<uint32_t>((size_t)count);
+  w.tensors = cv.take<GradRef>((size_t)count + 1);
+  w.parts = cv.take<GradPart>((size_t)parts);
   w.sums = cv.take<double>((size_t)count);
-  w.parts = cv.take<double>((size_t)parts);
+  w.partial = cv.take<double>((size_t)parts);
   return cv.off;
+}
+
+bool list_ok(const fp4root_grad_list* l) {
+  return l && l->mem && aligned(l->mem, kAlign) && l->count >= 0 && l->count <= kMaxTensors && l->parts >= l->count &&
+         l->parts <= l->count * 1024;
 }
 
 int check_clip(int kind, double max_norm, double eps, const void* total, const void* result) {
@@ -1530,26 +1526,56 @@ int check_clip(int kind, double max_norm, double eps, const void* total, const v
 
 extern "C" {
 
-size_t fp4root_grad_norm_workspace(const fp4root_tensor* tensors, int64_t count) {
-  if (check_tensors(tensors, count, false) != FP4ROOT_OK) return 0;
-  GradNormWs w;
-  return carve_grad_norm(nullptr, count, grad_parts(tensors, count), w);
+size_t fp4root_grad_list_size(const fp4root_tensor* tensors, int64_t count) {
+  if (count < 0 || count > kMaxTensors || (count > 0 && !tensors)) return 0;
+  const bool out = has_outputs(tensors, count);
+  if (check_tensors(tensors, count, out) != FP4ROOT_OK) return 0;
+  GradTable w;
+  return carve_grad_list(nullptr, count, grad_parts(tensors, count, out), w);
 }
 
-int fp4root_grad_norm(const fp4root_tensor* tensors, int64_t count, int kind, double max_norm, double eps,
-                      double* total, float* norms, float* result, void* ws, size_t ws_bytes, void* stream) {
-  FP4R_TRY_RC(check_tensors(tensors, count, false));
+int fp4root_grad_list_init(fp4root_grad_list* list, const fp4root_tensor* tensors, int64_t count, void* mem,
+                           size_t mem_bytes, void* stream) {
+  if (!list || count < 0 || count > kMaxTensors || (count > 0 && !tensors)) return FP4ROOT_ERR_INVALID_ARG;
+  const bool out = has_outputs(tensors, count);
+  FP4R_TRY_RC(check_tensors(tensors, count, out));
+  try {
+    if (out && !outputs_apart(tensors, count)) return FP4ROOT_ERR_INVALID_ARG;
+  } catch (const std::bad_alloc&) {
+    return FP4ROOT_ERR_HIP;
+  }
+  const int64_t parts = grad_parts(tensors, count, out);
+  if (parts > kMaxSharedBlocks) return FP4ROOT_ERR_SHAPE;   // more than the device's memory, or lists over the same
+  GradTable tb;
+  if (!mem || !aligned(mem, kAlign) || mem_bytes < carve_grad_list(mem, count, parts, tb)) return FP4ROOT_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  int64_t first = 0;
+  // one entry past the last: the number of parts
+  for (int64_t i0 = 0; i0 <= count; i0 += kMaxGradChunk) {
+    GradChunk ch;
+    ch.count = (int)std::min<int64_t>(kMaxGradChunk, count + 1 - i0);
+    for (int k = 0; k < ch.count; ++k) {
+      int64_t n = 0;
+      ch.t[k] = i0 + k < count ? grad_ref(tensors[i0 + k], out, n) : GradRef{};
+      ch.t[k].first = (uint32_t)first;
+      ch.parts[k] = (uint32_t)n;
+      first += n;
+    }
+    FP4R_TRY(launch_grad_table(ch, tb, (uint32_t)i0, st));
+  }
+  *list = fp4root_grad_list{mem, count, parts, out ? 1 : 0};
+  return FP4ROOT_OK;
+}
+
+int fp4root_grad_norm(const fp4root_grad_list* list, int kind, double max_norm, double eps, double* total,
+                      float* norms, float* result, void* stream) {
+  if (!list_ok(list)) return FP4ROOT_ERR_INVALID_ARG;
   FP4R_TRY_RC(check_clip(kind, max_norm, eps, total, result));
   if (!aligned(norms, 4)) return FP4ROOT_ERR_INVALID_ARG;
-  const int64_t parts = grad_parts(tensors, count);
-  GradNormWs w;
-  if (!ws || !aligned(ws, 8) || ws_bytes < carve_grad_norm(ws, count, parts, w)) return FP4ROOT_ERR_WORKSPACE;
-  hipStream_t st = (hipStream_t)stream;
-  const bool max = kind == FP4ROOT_NORM_MAX;
-  FP4R_TRY_RC(each_grad_chunk(tensors, count, false, [&](const GradChunk& ch, uint32_t part, uint32_t first) {
-    return launch_grad_parts(ch, w, part, first, max, st);
-  }));
-  FP4R_TRY(launch_grad_total(w, (uint32_t)count, (uint32_t)parts, max, max_norm, eps, total, norms, result, st));
+  GradTable tb;
+  carve_grad_list(list->mem, list->count, list->parts, tb);
+  FP4R_TRY(launch_grad_norm(tb, (uint32_t)list->count, (uint32_t)list->parts, kind == FP4ROOT_NORM_MAX, max_norm, eps,
+                            total, norms, result, (hipStream_t)stream));
   return FP4ROOT_OK;
 }
 
@@ -1559,17 +1585,14 @@ int fp4root_clip_coef(const double* total, int kind, double max_norm, double eps
   return FP4ROOT_OK;
 }
 
-int fp4root_clip_grads(const fp4root_tensor* tensors, int64_t count, const float* coef, void* stream) {
-  FP4R_TRY_RC(check_tensors(tensors, count, true));
-  if (!coef || !aligned(coef, 4)) return FP4ROOT_ERR_INVALID_ARG;
-  try {
-    if (!outputs_apart(tensors, count)) return FP4ROOT_ERR_INVALID_ARG;
-  } catch (const std::bad_alloc&) {
-    return FP4ROOT_ERR_HIP;
-  }
-  hipStream_t st = (hipStream_t)stream;
-  return each_grad_chunk(tensors, count, true,
-                         [&](const GradChunk& ch, uint32_t, uint32_t) { return launch_grad_scale(ch, coef, st); });
+int fp4root_clip_grads(const fp4root_grad_list* list, const float* coef, void* stream) {
+  if (!list_ok(list) || !coef || !aligned(coef, 4) || (list->count > 0 && !list->outputs))
+    return FP4ROOT_ERR_INVALID_ARG;
+  if (list->count == 0) return FP4ROOT_OK;
+  GradTable tb;
+  carve_grad_list(list->mem, list->count, list->parts, tb);
+  FP4R_TRY(launch_grad_scale(tb, (uint32_t)list->parts, coef, (hipStream_t)stream));
+  return FP4ROOT_OK;
 }
 
 namespace {

@@ -7,9 +7,10 @@
 // the clipping.  Both are bound by memory.
 //
 // A tensor is cut into parts of 16-byte vectors by its own size alone; a workgroup takes one
-// part and the workgroups of up to kMaxGradChunk tensors share a launch.  Every partial result
-// has its own place and the places are added in a fixed order, so a tensor's norm does not
-// change with the tensors beside it and nothing depends on the order of atomics.
+// part, found in a table that the list was given when it was made, so that any number of
+// tensors share a launch.  Every partial result has its own place and the places are added in a
+// fixed order, so a tensor's norm does not change with the tensors beside it and nothing
+// depends on the order of atomics.
 #include "device.h"
 #include "internal.h"
 #include "vec.h"
@@ -47,18 +48,6 @@ FP4R_DEV double block_join(double v) {
   return v;
 }
 
-// The tensor of a workgroup and its part (uniform).
-FP4R_DEV int find_part(const GradChunk& ch, uint32_t wg, uint32_t& part) {
-  int lo = 0, hi = ch.count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (wg < ch.end[mid]) hi = mid;
-    else lo = mid + 1;
-  }
-  part = wg - (lo ? ch.end[lo - 1] : 0u);
-  return lo;
-}
-
 // Calls f(first element's offset in the input, ... in the output, count) for every vector of
 // this thread in vectors [v0, v1) of the tensor; count is VE but for the last vector of a row.
 template <int VE, class F>
@@ -84,25 +73,29 @@ FP4R_DEV double part_value(const GradRef& t, int64_t v0, int64_t v1) {
   return acc;
 }
 
+// Writes a chunk of the table: workgroup i its tensor and that tensor's parts.
+__global__ __launch_bounds__(kThreads) void k_grad_table(GradChunk ch, GradTable tb, uint32_t first_tensor) {
+  const int i = blockIdx.x;
+  const uint32_t t = first_tensor + i;
+  if (threadIdx.x == 0) tb.tensors[t] = ch.t[i];
+  for (uint32_t p = threadIdx.x; p < ch.parts[i]; p += kThreads) tb.parts[ch.t[i].first + p] = GradPart{t, p};
+}
+
 template <bool MAX>
-__global__ __launch_bounds__(kThreads) void k_grad_parts(GradChunk ch, GradNormWs ws, uint32_t first_part,
-                                                         uint32_t first_tensor) {
-  uint32_t part;
-  const int i = find_part(ch, blockIdx.x, part);
-  const GradRef& t = ch.t[i];
-  const int64_t v0 = (int64_t)part << ch.shift[i], v1 = min(t.vectors, v0 + (int64_t(1) << ch.shift[i]));
+__global__ __launch_bounds__(kThreads) void k_grad_parts(GradTable tb) {
+  const GradPart p = tb.parts[blockIdx.x];
+  const GradRef& t = tb.tensors[p.tensor];
+  const int64_t v0 = (int64_t)p.part << t.shift, v1 = min(t.vectors, v0 + (int64_t(1) << t.shift));
   double v;
-  switch (ch.type[i] & 3) {
+  switch (t.type & 3) {
     case 0: v = part_value<float, MAX>(t, v0, v1); break;
     case 1: v = part_value<bf16_t, MAX>(t, v0, v1); break;
     default: v = part_value<f16_t, MAX>(t, v0, v1); break;
   }
   v = block_join<MAX>(v);
   if (threadIdx.x == 0) {
-    const uint32_t p = first_part + blockIdx.x;
-    ws.parts[p] = v;
-    if (part == 0) ws.first[first_tensor + i] = p;
-    if (p == 0) *ws.ticket = 0u;
+    tb.partial[blockIdx.x] = v;
+    if (blockIdx.x == 0) *tb.ticket = 0u;
   }
 }
 
@@ -113,33 +106,47 @@ FP4R_DEV void write_result(double total, bool max, double max_norm, double eps, 
   result[1] = q > 1.0 ? 1.0f : (float)q;   // a NaN stays
 }
 
-// One workgroup per tensor joins its parts; the last to finish joins the tensors.
+// A wave per tensor joins its parts (at most 1024); the last workgroup to finish joins the
+// tensors.  Up to kWaves tensors there is one workgroup, and nothing to wait for.
+constexpr int kWaves = 16;
 template <bool MAX>
-__global__ __launch_bounds__(kThreads) void k_grad_total(GradNormWs ws, uint32_t count, uint32_t parts, double max_norm,
-                                                         double eps, double* total, float* norms, float* result) {
+__global__ __launch_bounds__(kWaves * 64) void k_grad_total(GradTable tb, uint32_t count, double max_norm, double eps,
+                                                            double* total, float* norms, float* result) {
+  __shared__ double red[kWaves];
   __shared__ bool last;
-  if (count) {
-    const uint32_t t = blockIdx.x, p0 = ws.first[t], p1 = t + 1 < count ? ws.first[t + 1] : parts;
-    double v = 0.0;
-    for (uint32_t p = p0 + threadIdx.x; p < p1; p += kThreads) v = join<MAX>(v, ws.parts[p]);
-    v = block_join<MAX>(v);
-    if (threadIdx.x == 0) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t t = blockIdx.x * kWaves + wave;
+  double v = 0.0;
+  if (t < count) {
+    const uint32_t p0 = tb.tensors[t].first, p1 = tb.tensors[t + 1].first;
+    for (uint32_t p = p0 + lane; p < p1; p += 64) v = join<MAX>(v, tb.partial[p]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = join<MAX>(v, __shfl_xor(v, o));
+    if (lane == 0) {
       if (norms) norms[t] = (float)(MAX ? v : __builtin_sqrt(v));
-      __hip_atomic_store(&ws.sums[t], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last = __hip_atomic_fetch_add(ws.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == count - 1;
+      if (gridDim.x > 1) __hip_atomic_store(&tb.sums[t], v, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
     }
+  }
+  if (gridDim.x > 1) {
+    __syncthreads();
+    if (threadIdx.x == 0)
+      last = __hip_atomic_fetch_add(tb.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
     __syncthreads();
     if (!last) return;
+    v = 0.0;
+    for (uint32_t i = threadIdx.x; i < count; i += kWaves * 64)
+      v = join<MAX>(v, __hip_atomic_load(&tb.sums[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = join<MAX>(v, __shfl_xor(v, o));
   }
-  double v = 0.0;
-  for (uint32_t t = threadIdx.x; t < count; t += kThreads)
-    v = join<MAX>(v, __hip_atomic_load(&ws.sums[t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-  v = block_join<MAX>(v);
-  if (threadIdx.x == 0) {
-    *total = v;
-    write_result(v, MAX, max_norm, eps, result);
-    *ws.status = v < __builtin_inf() ? 0u : kStatusNonFinite;
-  }
+  if (lane == 0) red[wave] = v;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) v = join<MAX>(v, red[w]);
+  *total = v;
+  write_result(v, MAX, max_norm, eps, result);
+  *tb.status = v < __builtin_inf() ? 0u : kStatusNonFinite;
 }
 
 __global__ void k_clip_coef(const double* total, int max, double max_norm, double eps, float* result) {
@@ -160,14 +167,13 @@ FP4R_DEV void scale_part(const GradRef& t, int64_t v0, int64_t v1, float coef) {
   });
 }
 
-__global__ __launch_bounds__(kThreads) void k_grad_scale(GradChunk ch, const float* coef_p) {
-  uint32_t part;
-  const int i = find_part(ch, blockIdx.x, part);
-  const GradRef& t = ch.t[i];
+__global__ __launch_bounds__(kThreads) void k_grad_scale(GradTable tb, const float* coef_p) {
+  const GradPart p = tb.parts[blockIdx.x];
+  const GradRef& t = tb.tensors[p.tensor];
   const float coef = *coef_p;
   if (coef == 1.0f && t.in == t.out) return;   // in place, and x 1 is x
-  const int64_t v0 = (int64_t)part << ch.shift[i], v1 = min(t.vectors, v0 + (int64_t(1) << ch.shift[i]));
-  switch (ch.type[i]) {
+  const int64_t v0 = (int64_t)p.part << t.shift, v1 = min(t.vectors, v0 + (int64_t(1) << t.shift));
+  switch (t.type) {
     case 0 | 0 << 2: scale_part<float, float>(t, v0, v1, coef); break;
     case 0 | 1 << 2: scale_part<float, bf16_t>(t, v0, v1, coef); break;
     case 0 | 2 << 2: scale_part<float, f16_t>(t, v0, v1, coef); break;
@@ -182,25 +188,21 @@ __global__ __launch_bounds__(kThreads) void k_grad_scale(GradChunk ch, const flo
 
 }  // namespace
 
-hipError_t launch_grad_parts(const GradChunk& ch, const GradNormWs& ws, uint32_t first_part, uint32_t first_tensor,
-                             bool max, hipStream_t st) {
-  const dim3 grid(ch.end[ch.count - 1]);
-  if (max)
-    hipLaunchKernelGGL(k_grad_parts<true>, grid, dim3(kThreads), 0, st, ch, ws, first_part, first_tensor);
-  else
-    hipLaunchKernelGGL(k_grad_parts<false>, grid, dim3(kThreads), 0, st, ch, ws, first_part, first_tensor);
+hipError_t launch_grad_table(const GradChunk& ch, const GradTable& tb, uint32_t first_tensor, hipStream_t st) {
+  hipLaunchKernelGGL(k_grad_table, dim3(ch.count), dim3(kThreads), 0, st, ch, tb, first_tensor);
   return hipGetLastError();
 }
 
-hipError_t launch_grad_total(const GradNormWs& ws, uint32_t count, uint32_t parts, bool max, double max_norm, double eps,
-                             double* total, float* norms, float* result, hipStream_t st) {
-  const dim3 grid(count ? count : 1);
-  if (max)
-    hipLaunchKernelGGL(k_grad_total<true>, grid, dim3(kThreads), 0, st, ws, count, parts, max_norm, eps, total, norms,
-                       result);
-  else
-    hipLaunchKernelGGL(k_grad_total<false>, grid, dim3(kThreads), 0, st, ws, count, parts, max_norm, eps, total, norms,
-                       result);
+hipError_t launch_grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool max, double max_norm, double eps,
+                            double* total, float* norms, float* result, hipStream_t st) {
+  const dim3 groups(count ? (count + kWaves - 1) / kWaves : 1), nt(kWaves * 64);
+  if (max) {
+    if (parts) hipLaunchKernelGGL(k_grad_parts<true>, dim3(parts), dim3(kThreads), 0, st, tb);
+    hipLaunchKernelGGL(k_grad_total<true>, groups, nt, 0, st, tb, count, max_norm, eps, total, norms, result);
+  } else {
+    if (parts) hipLaunchKernelGGL(k_grad_parts<false>, dim3(parts), dim3(kThreads), 0, st, tb);
+    hipLaunchKernelGGL(k_grad_total<false>, groups, nt, 0, st, tb, count, max_norm, eps, total, norms, result);
+  }
   return hipGetLastError();
 }
 
@@ -209,8 +211,8 @@ hipError_t launch_clip_coef(const double* total, bool max, double max_norm, doub
   return hipGetLastError();
 }
 
-hipError_t launch_grad_scale(const GradChunk& ch, const float* coef, hipStream_t st) {
-  hipLaunchKernelGGL(k_grad_scale, dim3(ch.end[ch.count - 1]), dim3(kThreads), 0, st, ch, coef);
+hipError_t launch_grad_scale(const GradTable& tb, uint32_t parts, const float* coef, hipStream_t st) {
+  hipLaunchKernelGGL(k_grad_scale, dim3(parts), dim3(kThreads), 0, st, tb, coef);
   return hipGetLastError();
 }
 

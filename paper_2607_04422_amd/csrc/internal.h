@@ -388,34 +388,41 @@ struct QAdamWLaunch {
 hipError_t launch_qadamw(const QAdamWLaunch& p, hipStream_t st);
 
 // ---------------------------------------------------------------------------
-// Gradient lists (grads.hip): up to kMaxGradChunk tensors a launch, by value.
-constexpr int kMaxGradChunk = 64;
+// Gradient lists (grads.hip).
 struct GradRef {
   const void* in;
   void* out;
   int64_t rows, cols;      // one row where the tensor is contiguous
   int64_t ld_in, ld_out;
   int64_t vectors;         // of 16 bytes of the input: rows * ceil(cols / elements in 16 bytes)
+  uint16_t shift;          // log2 of the vectors in a part
+  uint16_t type;           // input type | output type << 2
+  uint32_t first;          // the tensor's first part among the list's
 };
+// A workgroup's work: part `part` of tensor `tensor`.
+struct GradPart {
+  uint32_t tensor, part;
+};
+// The table and the scratch behind a list.
+struct GradTable {
+  uint32_t *status, *ticket;
+  GradRef* tensors;        // one more than there are: the last holds the number of parts in `first`
+  GradPart* parts;
+  double *sums, *partial;
+};
+// Tensors by value, for the launches that write the table.
+constexpr int kMaxGradChunk = 48;
 struct GradChunk {
   GradRef t[kMaxGradChunk];
-  uint32_t end[kMaxGradChunk];    // parts up to and with tensor i
-  uint8_t shift[kMaxGradChunk];   // log2 of the vectors in a part
-  uint8_t type[kMaxGradChunk];    // input type | output type << 2
+  uint32_t parts[kMaxGradChunk];
   int count;
 };
-// Workspace of the norm: the first part of each tensor, and the sums of tensors and parts.
-struct GradNormWs {
-  uint32_t *status, *ticket, *first;
-  double *sums, *parts;
-};
-static_assert(sizeof(GradChunk) + sizeof(GradNormWs) + 8 <= 4096, "a launch's arguments");
-hipError_t launch_grad_parts(const GradChunk& ch, const GradNormWs& ws, uint32_t first_part, uint32_t first_tensor,
-                             bool max, hipStream_t st);
-hipError_t launch_grad_total(const GradNormWs& ws, uint32_t count, uint32_t parts, bool max, double max_norm, double eps,
-                             double* total, float* norms, float* result, hipStream_t st);
+static_assert(sizeof(GradChunk) + sizeof(GradTable) + 8 <= 4096, "a launch's arguments");
+hipError_t launch_grad_table(const GradChunk& ch, const GradTable& tb, uint32_t first_tensor, hipStream_t st);
+hipError_t launch_grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool max, double max_norm, double eps,
+                            double* total, float* norms, float* result, hipStream_t st);
 hipError_t launch_clip_coef(const double* total, bool max, double max_norm, double eps, float* result, hipStream_t st);
-hipError_t launch_grad_scale(const GradChunk& ch, const float* coef, hipStream_t st);
+hipError_t launch_grad_scale(const GradTable& tb, uint32_t parts, const float* coef, hipStream_t st);
 
 // ---------------------------------------------------------------------------
 // Root-mean-square norm (rmsnorm.hip).

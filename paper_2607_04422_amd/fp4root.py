@@ -70,6 +70,11 @@ class Tensor(ctypes.Structure):
                 ("in_type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
 
 
+class GradList(ctypes.Structure):
+    _fields_ = [("mem", ctypes.c_void_p), ("count", ctypes.c_int64), ("parts", ctypes.c_int64),
+                ("outputs", ctypes.c_int32)]
+
+
 class RmsNorm(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in
                 ("x", "residual", "gain", "h", "y", "codes", "scales", "rstd", "status")] + \
@@ -133,13 +138,15 @@ def load(path: str = None) -> ctypes.CDLL:
     lib.fp4root_root_step.argtypes = [ctypes.POINTER(Param), i64, ctypes.POINTER(RootConfig),
                                       ctypes.POINTER(NsConfig), vp, sz, vp]
     lib.fp4root_root_step.restype = ctypes.c_int
-    lib.fp4root_grad_norm_workspace.argtypes = [ctypes.POINTER(Tensor), i64]
-    lib.fp4root_grad_norm_workspace.restype = sz
-    lib.fp4root_grad_norm.argtypes = [ctypes.POINTER(Tensor), i64, ctypes.c_int, f64, f64, vp, vp, vp, vp, sz, vp]
+    lib.fp4root_grad_list_size.argtypes = [ctypes.POINTER(Tensor), i64]
+    lib.fp4root_grad_list_size.restype = sz
+    lib.fp4root_grad_list_init.argtypes = [ctypes.POINTER(GradList), ctypes.POINTER(Tensor), i64, vp, sz, vp]
+    lib.fp4root_grad_list_init.restype = ctypes.c_int
+    lib.fp4root_grad_norm.argtypes = [ctypes.POINTER(GradList), ctypes.c_int, f64, f64, vp, vp, vp, vp]
     lib.fp4root_grad_norm.restype = ctypes.c_int
     lib.fp4root_clip_coef.argtypes = [vp, ctypes.c_int, f64, f64, vp, vp]
     lib.fp4root_clip_coef.restype = ctypes.c_int
-    lib.fp4root_clip_grads.argtypes = [ctypes.POINTER(Tensor), i64, vp, vp]
+    lib.fp4root_clip_grads.argtypes = [ctypes.POINTER(GradList), vp, vp]
     lib.fp4root_clip_grads.restype = ctypes.c_int
     lib.fp4root_momentum_update_scaled.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp, f32, u32, u64, i32, vp, vp, sz,
                                                    vp]
@@ -487,7 +494,7 @@ class RootStep:
         if need == 0:
             raise ValueError("invalid parameters or configuration")
         self.ws = workspace(need, self.weights[0].device if n else torch.device("cuda"))
-        self.clipper = GradClipper(self.grads, max_norm) if max_norm is not None and n else None
+        self.clipper = GradClipper(self.grads, max_norm, measure_only=True) if max_norm is not None and n else None
 
     def __call__(self, step: int, stream=None, grad_scale: torch.Tensor = None):
         self.cfg.step = step
@@ -505,16 +512,16 @@ class RootStep:
         return fp4root_device_status(self.ws, stream)
 
 
-def _launch_stream(device, stream):
-    """The stream of a call on tensors of `device`: the given one, or the current one there."""
+def _launch_stream(device, stream) -> int:
+    """The raw stream of a call on tensors of `device`: the given one, or the current one there."""
     if stream is None:
-        return torch.cuda.current_stream(device)
+        return torch._C._cuda_getCurrentRawStream(device.index)
     if stream.device != device:
         raise ValueError("the stream belongs to another GPU than the tensors")
-    return stream
+    return stream.cuda_stream
 
 
-def _call(fn, device, *args):
+def _call(fn, device, *args) -> int:
     """fn(*args) with `device` current: kernels are launched on the current GPU's code."""
     if device.index != torch.cuda.current_device():
         with torch.cuda.device(device):
@@ -548,7 +555,7 @@ def _as_rows(t: torch.Tensor, name: str):
 class GradClipper:
     """The global norm of a fixed list of gradient tensors (float32, bfloat16 or float16, mixed
     as they come) and the clipping by it; see fp4root_grad_norm and fp4root_clip_grads in
-    include/fp4root.h.  Holds the descriptors, the workspace and the results:
+    include/fp4root.h.  Holds the list, its device memory and the results:
 
       total       float64 [1]: the sum of squares (norm_type 2) or largest magnitude (inf)
       norms       float32 [len(grads)]: each tensor's norm
@@ -557,16 +564,24 @@ class GradClipper:
     `norm()` computes these; a call computes them and multiplies every gradient by coef, into
     `outputs` (tensors of the gradients' shapes and any of the types, or None: in place).  Ranks
     that hold shards run `norm()`, all-reduce `total` (sum, or maximum for inf), then `recoef()`
-    and `scale()`.  RootStep, fp4root_qadamw_update and fp4root_momentum_update take `coef` as
-    grad_scale and then need no scaled gradients.  Each may be captured into a HIP graph; calls
-    of one GradClipper on two streams at once race.  Gradients must stay where they are.
+    and `scale()`.  With measure_only there is nothing to scale, and a tensor may be listed twice
+    (it counts twice).  RootStep, fp4root_qadamw_update and fp4root_momentum_update take `coef` as
+    grad_scale and then need no scaled gradients.  Each may be captured into a HIP graph, and
+    used on any stream once the object is made (it waits for its own set-up); calls of one
+    GradClipper on two streams at once race.  The gradients' memory must stay where it is.
     """
 
-    def __init__(self, grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6):
+    def __init__(self, grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6,
+                 measure_only: bool = False):
+        self._make(grads, max_norm, outputs, norm_type, eps, measure_only, None)
+        if self.count:
+            torch.cuda.current_stream(self.device).synchronize()
+
+    def _make(self, grads, max_norm, outputs, norm_type, eps, measure_only, stream):
         lib = load()
         self.grads = list(grads)
         self.outputs = list(outputs) if outputs is not None else self.grads
-        if len(self.outputs) != len(self.grads):
+        if len(self.outputs) != len(self.grads) or (measure_only and outputs is not None):
             raise ValueError("outputs must match grads")
         if norm_type not in (2, float("inf")):
             raise ValueError("norm_type must be 2 or inf")
@@ -574,37 +589,21 @@ class GradClipper:
             raise ValueError("max_norm must be positive and eps non-negative")
         self.kind = NORM_L2 if norm_type == 2 else NORM_MAX
         self.max_norm, self.eps = float(max_norm), float(eps)
-        n = len(self.grads)
-        self.tensors = (Tensor * max(n, 1))()
-        self.device = self.grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        n = self.count = len(self.grads)
+        tensors = (Tensor * max(n, 1))()
         for i, (g, o) in enumerate(zip(self.grads, self.outputs)):
             for name, t in ((f"grads[{i}]", g), (f"outputs[{i}]", o)):
-                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != self.device:
+                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != self.grads[0].device:
                     raise TypeError(f"{name} must be a tensor on the first gradient's GPU")
                 if t.dtype not in _TYPES:
                     raise TypeError(f"{name} must be float32, bfloat16 or float16")
             rows, cols, ld = _as_rows(g, f"grads[{i}]")
             ld_out = ld
             if o is not g:
-                if o.shape != g.shape:
-                    raise ValueError(f"outputs[{i}] must have the gradient's shape")
-                ri, ci, ld_out = _as_rows(o, f"outputs[{i}]")
-                order = [[t.stride(d) for d in range(t.dim()) if t.shape[d] > 1] for t in (g, o)]
-                if sorted(range(len(order[0])), key=order[0].__getitem__) != \
-                        sorted(range(len(order[1])), key=order[1].__getitem__):
-                    raise ValueError(f"outputs[{i}] must have its dimensions in memory in the gradient's order")
-                # a contiguous one beside one of rows is taken as those rows
-                if (ri, ci) != (rows, cols):
-                    if ri == 1 and rows * cols == ci:
-                        ld_out = cols
-                    elif rows == 1 and ri * ci == cols:
-                        rows, cols, ld = ri, ci, ci
-                    else:
-                        raise ValueError(f"outputs[{i}] must be laid out as the gradient, or contiguous")
-            self.tensors[i] = Tensor(g.data_ptr(), o.data_ptr(), rows, cols, ld, ld_out, _TYPES[g.dtype],
-                                     _TYPES[o.dtype])
-        self.count = n
-        need = lib.fp4root_grad_norm_workspace(self.tensors, n)
+                rows, cols, ld, ld_out = _rows_of_both(g, o, rows, cols, ld, i)
+            tensors[i] = Tensor(g.data_ptr(), None if measure_only else o.data_ptr(), rows, cols, ld, ld_out, _TYPES[g.dtype], _TYPES[o.dtype])
+        self.device = self.grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        need = lib.fp4root_grad_list_size(tensors, n)
         if need == 0:
             raise ValueError("invalid gradients")
         self.ws = workspace(need, self.device)
@@ -612,29 +611,29 @@ class GradClipper:
         self.norms = torch.zeros(n, dtype=torch.float32, device=self.device)
         self.result = torch.zeros(2, dtype=torch.float32, device=self.device)
         self.total_norm, self.coef = self.result[0], self.result[1]
-        self._args = (_ptr(self.total), _ptr(self.norms) if n else None, _ptr(self.result), _ptr(self.ws),
-                      self.ws.numel())
-        self._coef = _ptr(self.coef)
+        self.list = GradList()
+        _check(_call(lib.fp4root_grad_list_init, self.device, ctypes.byref(self.list), tensors, n, _ptr(self.ws),
+                     self.ws.numel(), _launch_stream(self.device, stream)), "fp4root_grad_list_init")
+        self._list = ctypes.byref(self.list)
+        self._norm_args = (self._list, self.kind, self.max_norm, self.eps, _ptr(self.total),
+                           _ptr(self.norms) if n else None, _ptr(self.result))
 
     def norm(self, stream=None) -> torch.Tensor:
         """The norm (self.total_norm), and with it total, norms and coef."""
-        s = _launch_stream(self.device, stream).cuda_stream
-        _check(_call(load().fp4root_grad_norm, self.device, self.tensors, self.count, self.kind, self.max_norm,
-                     self.eps, *self._args, s), "fp4root_grad_norm")
+        _check(_call(_lib.fp4root_grad_norm, self.device, *self._norm_args, _launch_stream(self.device, stream)),
+               "fp4root_grad_norm")
         return self.total_norm
 
     def recoef(self, stream=None) -> torch.Tensor:
         """total_norm and coef again, from `total` (after an all-reduce)."""
-        s = _launch_stream(self.device, stream).cuda_stream
-        _check(_call(load().fp4root_clip_coef, self.device, self._args[0], self.kind, self.max_norm, self.eps,
-                     self._args[2], s), "fp4root_clip_coef")
+        _check(_call(_lib.fp4root_clip_coef, self.device, _ptr(self.total), self.kind, self.max_norm, self.eps,
+                     _ptr(self.result), _launch_stream(self.device, stream)), "fp4root_clip_coef")
         return self.total_norm
 
     def scale(self, stream=None):
         """Every gradient times coef, into the outputs, which it returns."""
-        s = _launch_stream(self.device, stream).cuda_stream
-        _check(_call(load().fp4root_clip_grads, self.device, self.tensors, self.count, self._coef, s),
-               "fp4root_clip_grads")
+        _check(_call(_lib.fp4root_clip_grads, self.device, self._list, _ptr(self.coef),
+                     _launch_stream(self.device, stream)), "fp4root_clip_grads")
         return self.outputs
 
     def __call__(self, stream=None):
@@ -643,18 +642,38 @@ class GradClipper:
 
     def status(self, stream=None) -> int:
         """FP4ROOT_ERR_NONFINITE where the last norm met a NaN or an infinity, else 0 (waits)."""
-        return fp4root_device_status(self.ws, _launch_stream(self.device, stream))
+        return _call(_lib.fp4root_device_status, self.device, _ptr(self.ws), _launch_stream(self.device, stream))
+
+
+def _rows_of_both(g, o, rows, cols, ld, i):
+    """(rows, cols, row stride, output's row stride) under which both are walked alike."""
+    if o.shape != g.shape:
+        raise ValueError(f"outputs[{i}] must have the gradient's shape")
+    ri, ci, ld_out = _as_rows(o, f"outputs[{i}]")
+    dims = [d for d in range(g.dim()) if g.shape[d] > 1]
+    if sorted(dims, key=lambda d: g.stride(d)) != sorted(dims, key=lambda d: o.stride(d)):
+        raise ValueError(f"outputs[{i}] must have its dimensions in memory in the gradient's order")
+    if (ri, ci) != (rows, cols):       # a contiguous one beside one of rows is taken as those rows
+        if ri == 1 and rows * cols == ci:
+            ld_out = cols
+        elif rows == 1 and ri * ci == cols:
+            rows, cols, ld = ri, ci, ci
+        else:
+            raise ValueError(f"outputs[{i}] must be laid out as the gradient, or contiguous")
+    return rows, cols, ld, ld_out
 
 
 def fp4root_clip_grads(grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6, stream=None):
     """Clip a list of gradient tensors by their global norm, in place or into `outputs`; returns
     the norm before clipping (a float32 GPU scalar).  A program that clips the same buffers step
     after step keeps a GradClipper instead."""
-    c = GradClipper(grads, max_norm, outputs, norm_type, eps)
-    c(stream)
-    if stream is not None:                 # the results were allocated on the current stream
+    c = GradClipper.__new__(GradClipper)
+    c._make(grads, max_norm, outputs, norm_type, eps, False, stream)
+    if stream is not None:                 # the memory was allocated, and cleared, on the current stream
         for t in (c.ws, c.total, c.norms, c.result):
             t.record_stream(stream)
+        stream.wait_stream(torch.cuda.current_stream(c.device))
+    c(stream)
     return c.total_norm
 
 
@@ -706,6 +725,7 @@ def _gain_type(gain, x):
 
 
 def _need_stream(x, name: str):
+    load()
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if x.dtype not in _TYPES:
@@ -724,65 +744,51 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     (h may be the residual or x itself: in place); status: an int32 GPU tensor of one element.
     See fp4root_rmsnorm_quantize in include/fp4root.h."""
     _need_stream(x, "x")
-    a = RmsNorm()
-    a.type, a.gain_type = _TYPES[x.dtype], _gain_type(gain, x)
-    a.rows, a.ld_x = _matrix(x, "x")
-    cols = a.cols = x.shape[-1]
-    dev = x.device
-    a.x = x.data_ptr()
-    if gain is not None:
-        a.gain = gain.data_ptr()
-    if residual is not None:
-        a.ld_residual = _matrix(residual, "residual", x)[1]
-        a.residual = residual.data_ptr()
-    a.group, a.scale_type, a.eps = group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps
-    lead = x.shape[:-1]
-    stream_ = _launch_stream(dev, stream)
+    gain_type = _gain_type(gain, x)
+    rows, ld_x = _matrix(x, "x")
+    shape, dev = x.shape, x.device
+    lead, cols = shape[:-1], shape[-1]
+    ld_r = _matrix(residual, "residual", x)[1] if residual is not None else 0
+    raw = _launch_stream(dev, stream)
     if out is None:
         codes = scales = y = None
+        packed = x.is_contiguous()         # empty_like keeps a stride, and is the cheaper call
         if quantize:
-            codes = torch.empty(x.shape, dtype=torch.uint8, device=dev)
-            shape = (*lead, -(-cols // group)) if group > 0 else lead
-            scales = torch.empty(shape, dtype=torch.uint8 if e8m0 else torch.float32, device=dev)
-        rstd = torch.empty(lead, dtype=torch.float32, device=dev)
-        h = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device=dev)
+            codes = torch.empty_like(x, dtype=torch.uint8) if packed else x.new_empty(shape, dtype=torch.uint8)
+            scales = x.new_empty((*lead, -(-cols // group)) if group > 0 else lead,
+                                 dtype=torch.uint8 if e8m0 else torch.float32)
+        rstd = x.new_empty(lead, dtype=torch.float32)
+        h = x if residual is None else torch.empty_like(x) if packed else x.new_empty(shape)
         if want_y:
-            y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+            y = x.new_empty(shape)
         out = RmsNormOutput(codes, scales, rstd, h, y)
+        ld_h = ld_y = cols
         if stream is not None:
             for t in out:
                 if t is not None and t is not x:
                     t.record_stream(stream)
     else:
         codes, scales, rstd, h, y = out
-        for name, t, dtype, shape in (("codes", codes, torch.uint8, x.shape),
-                                      ("scales", scales, torch.uint8 if e8m0 else torch.float32,
-                                       (*lead, -(-cols // group)) if group > 0 else tuple(lead)),
-                                      ("rstd", rstd, torch.float32, lead)):
-            if t is None:
-                continue
-            if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != dev:
-                raise ValueError(f"out.{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on x's GPU")
-    if residual is None:
-        out = out._replace(h=x)            # the stream is x: nothing to write
-    elif h is not None:
-        a.ld_h = _matrix(h, "out.h", x)[1]
-        a.h = h.data_ptr()
-    if y is not None:
-        a.ld_y = _matrix(y, "out.y", x)[1]
-        a.y = y.data_ptr()
-    if codes is not None:
-        a.codes = codes.data_ptr()
-    if scales is not None:
-        a.scales = scales.data_ptr()
-    if rstd is not None:
-        a.rstd = rstd.data_ptr()
-    if status is not None:
-        if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
-            raise ValueError("status must be one int32 element on x's GPU")
-        a.status = status.data_ptr()
-    _check(_call(load().fp4root_rmsnorm_quantize, dev, ctypes.byref(a), stream_.cuda_stream),
-           "fp4root_rmsnorm_quantize")
+        for name, t, dtype, want in (("codes", codes, torch.uint8, shape),
+                                     ("scales", scales, torch.uint8 if e8m0 else torch.float32,
+                                      (*lead, -(-cols // group)) if group > 0 else lead),
+                                     ("rstd", rstd, torch.float32, lead)):
+            if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(want) or not t.is_contiguous() or
+                                  t.device != dev):
+                raise ValueError(f"out.{name} must be a contiguous {dtype} tensor of shape {tuple(want)} on x's GPU")
+        if residual is None and h is not x:
+            out = out._replace(h=x)        # the stream is x: nothing to write
+        ld_h = _matrix(h, "out.h", x)[1] if residual is not None and h is not None else 0
+        ld_y = _matrix(y, "out.y", x)[1] if y is not None else 0
+    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.device != dev):
+        raise ValueError("status must be one int32 element on x's GPU")
+    a = RmsNorm(x.data_ptr(), residual.data_ptr() if residual is not None else None, gain.data_ptr() if gain is not None else None,
+                h.data_ptr() if residual is not None and h is not None else None,
+                y.data_ptr() if y is not None else None, codes.data_ptr() if codes is not None else None,
+                scales.data_ptr() if scales is not None else None, rstd.data_ptr() if rstd is not None else None,
+                status.data_ptr() if status is not None else None, rows, cols, ld_x, ld_r, ld_h, ld_y, _TYPES[x.dtype],
+                gain_type, group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps)
+    _check(_call(_lib.fp4root_rmsnorm_quantize, dev, ctypes.byref(a), raw), "fp4root_rmsnorm_quantize")
     return out
 
 
@@ -801,31 +807,36 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     _need_gpu_f32(rstd, "rstd")
     if rstd.numel() != rows or not rstd.is_contiguous() or rstd.device != dev:
         raise ValueError("rstd must hold one contiguous element per row on h's GPU")
-    stream_ = _launch_stream(dev, stream)
+    raw = _launch_stream(dev, stream)
     new = []
     if dx is None:
-        dx = torch.empty(h.shape, dtype=h.dtype, device=dev)
+        dx = torch.empty_like(h) if h.is_contiguous() else h.new_empty(h.shape)
+        ld_dx = cols
         new.append(dx)
-    ld_dx = _matrix(dx, "dx", h)[1]
+    else:
+        ld_dx = _matrix(dx, "dx", h)[1]
     need = 0
     if dgain is None and want_dgain:
-        dgain = torch.empty(cols, dtype=torch.float32, device=dev)
+        dgain = h.new_empty(cols, dtype=torch.float32)
         new.append(dgain)
     if dgain is not None:
         _need_gpu_f32(dgain, "dgain")
         if dgain.numel() != cols or not dgain.is_contiguous() or dgain.device != dev:
             raise ValueError("dgain must hold one contiguous element per column on h's GPU")
-        need = load().fp4root_rmsnorm_backward_workspace(rows, cols)
-        if ws is None or ws.numel() < need:
-            ws = workspace(need, dev)
+        need = _lib.fp4root_rmsnorm_backward_workspace(rows, cols)
+        if ws is None:
+            ws = h.new_empty(need, dtype=torch.uint8)
             new.append(ws)
+        elif ws.device != dev or not ws.is_contiguous():
+            raise ValueError("ws must be contiguous on h's GPU")
     if stream is not None:
         for t in new:
             t.record_stream(stream)
-    _check(_call(load().fp4root_rmsnorm_backward, dev, _ptr(dy), ld_dy, _ptr(h), ld_h, _ptr(dh), ld_dh, _ptr(gain),
-                 _ptr(rstd), _ptr(dx), ld_dx, _ptr(dgain), rows, cols, _TYPES[h.dtype], gain_type,
-                 _ptr(ws) if need else None, ws.numel() if need else 0, stream_.cuda_stream),
-           "fp4root_rmsnorm_backward")
+    _check(_call(_lib.fp4root_rmsnorm_backward, dev, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h,
+                 dh.data_ptr() if dh is not None else None, ld_dh, gain.data_ptr() if gain is not None else None,
+                 rstd.data_ptr(), dx.data_ptr(), ld_dx, dgain.data_ptr() if dgain is not None else None, rows, cols,
+                 _TYPES[h.dtype], gain_type, ws.data_ptr() if need else None,
+                 ws.numel() * ws.element_size() if need else 0, raw), "fp4root_rmsnorm_backward")
     return dx, dgain
 
 

@@ -1,4 +1,5 @@
-"""Gradient norm and clipping (fp4root_grad_norm, fp4root_clip_coef, fp4root_clip_grads) and the
+"""Gradient norm and clipping (fp4root_grad_list_*, fp4root_grad_norm,
+fp4root_clip_coef, fp4root_clip_grads) and the
 optimizer steps that read gradients through the clipping coefficient.
 
 Tolerances.  A total is a binary64 sum of exact squares: any order of n additions is within
@@ -86,6 +87,18 @@ def test_norm_and_clip(name, dtype, kind):
         assert c.status() == 0
 
 
+def test_mixed_types_and_many_tensors():
+    """Types side by side in one list, and more tensors than one workgroup joins."""
+    for n in (15, 16, 17, 47, 48, 49, 1100):
+        grads = [make([(1 + 61 * (i % 23), 3)], TYPES[i % 3], i)[0] for i in range(n)]
+        want = [g.clone() for g in grads]
+        for kind in (2, math.inf):
+            c = F.GradClipper(grads, 0.3, norm_type=kind, outputs=[torch.zeros_like(g, dtype=torch.float32) for g in grads])
+            for g, o in zip(want, c()):
+                assert torch.equal(o, g.float() * c.coef)
+            check(c, want, kind)
+
+
 @pytest.mark.parametrize("out", TYPES)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_clip_types(dtype, out):
@@ -140,7 +153,14 @@ def test_rows_beside_contiguous():
         with pytest.raises(ValueError):
             F.GradClipper(grads[:1], 0.5, outputs=[bad])
     with pytest.raises(F.Fp4RootError):
-        F.GradClipper([grads[1], grads[1]], 0.5)()
+        F.GradClipper([grads[1], grads[1]], 0.5)
+    with pytest.raises(ValueError):
+        F.GradClipper(grads, 0.5, outputs=outs, measure_only=True)
+    twice = F.GradClipper([grads[1], grads[1]], 0.5, measure_only=True)
+    twice.norm()
+    check(twice, [grads[1], grads[1]])
+    with pytest.raises(F.Fp4RootError):
+        twice.scale()
 
 
 def test_extremes_of_the_type():

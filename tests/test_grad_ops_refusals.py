@@ -22,50 +22,58 @@ def array(*ts):
     return (F.Tensor * max(len(ts), 1))(*ts)
 
 
-def norm(ts, count=None, kind=0, max_norm=1.0, eps=1e-6, total=Q, result=Q + 64, ws=WS, ws_bytes=1 << 20, norms=None):
-    return F.load().fp4root_grad_norm(array(*ts), len(ts) if count is None else count, kind, max_norm, eps, total, norms,
-                                      result, ws, ws_bytes, None)
+def init(*ts, count=None, mem=WS, mem_bytes=1 << 20):
+    """An init that has to fail: what would pass the checks has no GPU to run on."""
+    out = F.GradList()
+    rc = F.load().fp4root_grad_list_init(ctypes.byref(out), array(*ts), len(ts) if count is None else count, mem, mem_bytes,
+                                         None)
+    assert out.mem is None
+    return rc
 
 
-def clip(*ts, coef=WS):
-    return F.load().fp4root_clip_grads(array(*ts), len(ts), coef, None)
+def test_list_refusals():
+    t = tensor()
+    assert F.load().fp4root_grad_list_init(None, array(t), 1, WS, 1 << 20, None) == -1
+    assert init(t, count=-1) == -1
+    assert init(t, count=(1 << 20) + 1) == -1
+    assert init(t, mem=None) == -3
+    assert init(t, mem=WS + 128) == -3
+    assert init(t, mem_bytes=F.load().fp4root_grad_list_size(array(t), 1) - 1) == -3
+    for bad, rc in ((dict(in_type=3), -1), (dict(rows=-1), -2), (dict(cols=1 << 37), -2),
+                    (dict(rows=1 << 20, cols=1 << 20, ld_in=1 << 20), -2), (dict(ld_in=63), -2), (dict(ld_in=1 << 40), -2),
+                    (dict(in_=None), -1), (dict(in_=P + 2), -1), (dict(in_=P + 1, in_type=1), -1),
+                    (dict(out=None, in_=None), -1)):
+        assert init(tensor(**bad)) == rc, bad
+        assert init(t, tensor(**bad)) == rc, bad             # every tensor is checked
+        assert F.load().fp4root_grad_list_size(array(tensor(**bad)), 1) == 0
+    assert init(t, tensor(in_=P + 0x10000, out=None)) == -1  # outputs for all or for none
+
+
+def test_list_size():
+    lib = F.load()
+    assert lib.fp4root_grad_list_size(array(), 0) > 0
+    assert lib.fp4root_grad_list_size(array(tensor(rows=0, in_=None, out=None)), 1) > 0
+    # at most 1024 parts a tensor
+    big = lib.fp4root_grad_list_size(array(tensor(rows=1, cols=1 << 36, out=None)), 1)
+    assert big <= 6 * 256 + 1024 * 16
 
 
 def test_norm_refusals():
-    t = tensor()
-    assert norm([t], count=-1) == -1
-    assert norm([t], count=(1 << 20) + 1) == -1
-    assert norm([t], kind=2) == -1
-    for bad in (0.0, -1.0, NAN):
-        assert norm([t], max_norm=bad) == -1
-    for bad in (-1e-6, NAN, INF):
-        assert norm([t], eps=bad) == -1
-    assert norm([t], total=None) == -1
-    assert norm([t], total=Q + 4) == -1
-    assert norm([t], result=None) == -1
-    assert norm([t], norms=Q + 2) == -1
-    assert norm([t], ws=None) == -3
-    assert norm([t], ws_bytes=F.load().fp4root_grad_norm_workspace(array(t), 1) - 1) == -3
-    assert norm([tensor(in_type=3)]) == -1
-    assert norm([tensor(rows=-1)]) == -2
-    assert norm([tensor(cols=1 << 37)]) == -2
-    assert norm([tensor(rows=1 << 20, cols=1 << 20, ld_in=1 << 20)]) == -2
-    assert norm([tensor(ld_in=63)]) == -2
-    assert norm([tensor(ld_in=1 << 40)]) == -2
-    assert norm([tensor(in_=None)]) == -1
-    assert norm([tensor(in_=P + 2)]) == -1
-    assert norm([tensor(in_=P + 1, in_type=1)]) == -1
-    assert norm([t, tensor(in_type=7)]) == -1        # every tensor is checked
-
-
-def test_norm_workspace():
     lib = F.load()
-    assert lib.fp4root_grad_norm_workspace(array(), 0) > 0
-    assert lib.fp4root_grad_norm_workspace(array(tensor(ld_in=3)), 1) == 0
-    assert lib.fp4root_grad_norm_workspace(array(tensor(rows=0, in_=None)), 1) > 0
-    # at most 1024 partial sums a tensor
-    big = lib.fp4root_grad_norm_workspace(array(tensor(rows=1, cols=1 << 36)), 1)
-    assert big <= 5 * 256 + 1024 * 8
+    good = F.GradList(WS, 3, 5, 1)
+
+    def norm(lst=good, kind=0, max_norm=1.0, eps=1e-6, total=Q, result=Q + 64, norms=None):
+        return lib.fp4root_grad_norm(ctypes.byref(lst) if lst else None, kind, max_norm, eps, total, norms, result, None)
+    for bad in (0.0, -1.0, NAN):
+        assert norm(max_norm=bad) == -1
+    for bad in (-1e-6, NAN, INF):
+        assert norm(eps=bad) == -1
+    for kw in (dict(lst=None), dict(lst=F.GradList()), dict(lst=F.GradList(WS + 4, 3, 5, 1)), dict(lst=F.GradList(WS, 3, 2, 1)),
+               dict(lst=F.GradList(WS, 3, 4000, 1)), dict(kind=2), dict(total=None), dict(total=Q + 4), dict(result=None),
+               dict(norms=Q + 2)):
+        assert norm(**kw) == -1, kw
+    for lst, coef in ((good, None), (good, Q + 2), (F.GradList(WS, 3, 5, 0), Q), (F.GradList(), Q)):
+        assert lib.fp4root_clip_grads(ctypes.byref(lst), coef, None) == -1
 
 
 def test_clip_coef_refusals():
@@ -78,25 +86,23 @@ def test_clip_coef_refusals():
 
 def test_clip_refuses_overlaps():
     """An output may be its own input and nothing else: workgroups run side by side."""
-    assert clip(tensor(), coef=None) == -1
-    assert clip(tensor(out=None)) == -1
-    assert clip(tensor(out_type=9)) == -1
-    assert clip(tensor(out=Q + 2)) == -1
-    assert clip(tensor(ld_out=8)) == -2
-    assert clip(tensor(out=P, out_type=1)) == -1                    # in place under another type
-    assert clip(tensor(out=P, ld_out=128)) == -1                    # ... another stride
-    assert clip(tensor(out=P + 64)) == -1                           # partly over itself
+    assert init(tensor(out_type=9)) == -1
+    assert init(tensor(out=Q + 2)) == -1
+    assert init(tensor(ld_out=8)) == -2
+    assert init(tensor(out=P, out_type=1)) == -1                    # in place under another type
+    assert init(tensor(out=P, ld_out=128)) == -1                    # ... another stride
+    assert init(tensor(out=P + 64)) == -1                           # partly over itself
     one = tensor(out=P)
-    assert clip(one, one) == -1                                     # listed twice
-    assert clip(tensor(out=P), tensor(in_=P, out=Q)) == -1          # read while written
-    assert clip(tensor(out=Q), tensor(in_=P, out=Q + 128)) == -1    # two outputs
+    assert init(one, one) == -1                                     # listed twice
+    assert init(tensor(out=P), tensor(in_=P, out=Q)) == -1          # read while written
+    assert init(tensor(out=Q), tensor(in_=P, out=Q + 128)) == -1    # two outputs
     # columns 0..31 and 16..47 of one matrix with row stride 64
     a = tensor(in_=P, out=P, cols=32)
-    assert clip(a, tensor(in_=P + 64, out=P + 64, cols=32)) == -1
+    assert init(a, tensor(in_=P + 64, out=P + 64, cols=32)) == -1
     # wrapping into the next row's first columns
-    assert clip(a, tensor(in_=P + 128 + 4, out=P + 128 + 4, cols=32)) == -1
+    assert init(a, tensor(in_=P + 128 + 4, out=P + 128 + 4, cols=32)) == -1
     # a vector inside the matrix's columns
-    assert clip(a, tensor(in_=P + 256, out=P + 256, rows=1, cols=8)) == -1
+    assert init(a, tensor(in_=P + 256, out=P + 256, rows=1, cols=8)) == -1
 
 
 def rms(**kw):
