@@ -1503,7 +1503,6 @@ int64_t grad_parts(const fp4root_tensor* t, int64_t count, bool out) {
 size_t carve_grad_list(void* base, int64_t count, int64_t parts, GradTable& w) {
   Carver cv(base);
   w.status = cv.take<uint32_t>(1);
-  w.ticket = cv.take<uint32_t>(1);
   w.tensors = cv.take<GradRef>((size_t)count + 1);
   w.parts = cv.take<GradPart>((size_t)parts);
   w.sums = cv.take<double>((size_t)count);

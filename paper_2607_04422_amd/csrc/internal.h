@@ -405,7 +405,7 @@ struct GradPart {
 };
 // The table and the scratch behind a list.
 struct GradTable {
-  uint32_t *status, *ticket;
+  uint32_t* status;
   GradRef* tensors;        // one more than there are: the last holds the number of parts in `first`
   GradPart* parts;
   double *sums, *partial;

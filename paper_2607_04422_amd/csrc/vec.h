@@ -40,30 +40,30 @@ FP4R_DEV uint32_t f16_bits(float v) {
 FP4R_DEV uint32_t pack2(bf16_t, float a, float b) { return bf16_pair(a, b); }
 FP4R_DEV uint32_t pack2(f16_t, float a, float b) { return f16_bits(a) | f16_bits(b) << 16; }
 
-// N values from N / 4 or N / 8 vectors of 16 bytes (4 or 8 elements; N = 4 of a 16-bit type:
-// one of 8 bytes).
+// A vector of N elements as it lies in memory (8 or 16 bytes), and its values.
 template <class T, int N>
-FP4R_DEV void load_full(const T* p, float (&x)[N]) {
+FP4R_DEV auto load_raw(const T* p) {
+  static_assert(N * sizeof(T) == 16 || (N * sizeof(T) == 8 && sizeof(T) == 2), "one vector");
   if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int q = 0; q < N / 4; ++q) {
-      const u32x4 w = *reinterpret_cast<const u32x4_a4*>(p + 4 * q);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[4 * q + k] = __uint_as_float(w[k]);
-    }
-  } else if constexpr (N == 4) {
-    const u32x2 w = *reinterpret_cast<const u32x2_a2*>(p);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) unpack2(T{}, w[k], x[2 * k], x[2 * k + 1]);
+    const u32x4 w = *reinterpret_cast<const u32x4_a4*>(p);
+    return w;
+  } else if constexpr (N == 8) {
+    const u32x4 w = *reinterpret_cast<const u32x4_a2*>(p);
+    return w;
   } else {
-#pragma unroll
-    for (int q = 0; q < N / 8; ++q) {
-      const u32x4 w = *reinterpret_cast<const u32x4_a2*>(p + 8 * q);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) unpack2(T{}, w[k], x[8 * q + 2 * k], x[8 * q + 2 * k + 1]);
-    }
+    const u32x2 w = *reinterpret_cast<const u32x2_a2*>(p);
+    return w;
   }
 }
+template <class T, int N, class V>
+FP4R_DEV void unpack_raw(const V& w, float (&x)[N]) {
+#pragma unroll
+  for (int k = 0; k < (int)(N * sizeof(T) / 4); ++k) {
+    if constexpr (sizeof(T) == 4) x[k] = __uint_as_float(w[k]);
+    else unpack2(T{}, w[k], x[2 * k], x[2 * k + 1]);
+  }
+}
+// N values as 16-byte vectors (4 of a 16-bit type: one of 8 bytes).
 template <class T, int N>
 FP4R_DEV void store_full(T* p, const float (&x)[N]) {
   if constexpr (sizeof(T) == 4) {
@@ -94,7 +94,7 @@ FP4R_DEV void store_full(T* p, const float (&x)[N]) {
 template <class T, int N>
 FP4R_DEV void load_vec(const T* p, int n, float (&x)[N]) {
   if (n >= N) {
-    load_full<T, N>(p, x);
+    unpack_raw<T, N>(load_raw<T, N>(p), x);
   } else {
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = k < n ? to_f32(p[k]) : 0.0f;

@@ -89,7 +89,7 @@ def test_norm_and_clip(name, dtype, kind):
 
 def test_mixed_types_and_many_tensors():
     """Types side by side in one list, and more tensors than one workgroup joins."""
-    for n in (15, 16, 17, 47, 48, 49, 1100):
+    for n in (15, 16, 17, 47, 48, 49, 63, 64, 65, 1100):
         grads = [make([(1 + 61 * (i % 23), 3)], TYPES[i % 3], i)[0] for i in range(n)]
         want = [g.clone() for g in grads]
         for kind in (2, math.inf):
