@@ -351,7 +351,7 @@ typedef struct {
 typedef struct {
   void* mem;
   int64_t count, parts;
-  int32_t outputs;   /* whether the tensors have outputs */
+  int32_t flags, reserved;
 } fp4root_grad_list;
 
 /* Device bytes of a list of `count` tensors (host array, at most 2^20), or 0 for an invalid one. */

@@ -419,10 +419,11 @@ struct GradChunk {
 };
 static_assert(sizeof(GradChunk) + sizeof(GradTable) + 8 <= 4096, "a launch's arguments");
 hipError_t launch_grad_table(const GradChunk& ch, const GradTable& tb, uint32_t first_tensor, hipStream_t st);
-hipError_t launch_grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool max, double max_norm, double eps,
-                            double* total, float* norms, float* result, hipStream_t st);
+// past: read past the caches.
+hipError_t launch_grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool past, bool max, double max_norm,
+                            double eps, double* total, float* norms, float* result, hipStream_t st);
 hipError_t launch_clip_coef(const double* total, bool max, double max_norm, double eps, float* result, hipStream_t st);
-hipError_t launch_grad_scale(const GradTable& tb, uint32_t parts, const float* coef, hipStream_t st);
+hipError_t launch_grad_scale(const GradTable& tb, uint32_t parts, bool past, const float* coef, hipStream_t st);
 
 // ---------------------------------------------------------------------------
 // Root-mean-square norm (rmsnorm.hip).

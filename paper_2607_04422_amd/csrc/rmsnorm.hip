@@ -337,7 +337,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_rms_bwd(RmsBwdArgs a)
           for (int q = 1; q < RPG; ++q) acc[i][k] += slab[(q * 8 + k) * TPR + t];
       }
     }
-    if (slot == 0 && n > 0) store_vec<float, 8>(out + c, n, acc[i]);
+    if (slot == 0 && n > 0) store_raw8(out + c, n, pack8<float>(acc[i]));
   }
 }
 

@@ -40,20 +40,19 @@ FP4R_DEV uint32_t f16_bits(float v) {
 FP4R_DEV uint32_t pack2(bf16_t, float a, float b) { return bf16_pair(a, b); }
 FP4R_DEV uint32_t pack2(f16_t, float a, float b) { return f16_bits(a) | f16_bits(b) << 16; }
 
-// A vector of N elements as it lies in memory (8 or 16 bytes), and its values.
-template <class T, int N>
+// A vector of N elements as it lies in memory (8 or 16 bytes), and its values.  NT: past the
+// caches, which keep what they hold.
+template <bool NT, class V, class P>
+FP4R_DEV V load_as(const P* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <class T, int N, bool NT = false>
 FP4R_DEV auto load_raw(const T* p) {
   static_assert(N * sizeof(T) == 16 || (N * sizeof(T) == 8 && sizeof(T) == 2), "one vector");
-  if constexpr (sizeof(T) == 4) {
-    const u32x4 w = *reinterpret_cast<const u32x4_a4*>(p);
-    return w;
-  } else if constexpr (N == 8) {
-    const u32x4 w = *reinterpret_cast<const u32x4_a2*>(p);
-    return w;
-  } else {
-    const u32x2 w = *reinterpret_cast<const u32x2_a2*>(p);
-    return w;
-  }
+  if constexpr (sizeof(T) == 4) return load_as<NT, u32x4>(reinterpret_cast<const u32x4_a4*>(p));
+  else if constexpr (N == 8) return load_as<NT, u32x4>(reinterpret_cast<const u32x4_a2*>(p));
+  else return load_as<NT, u32x2>(reinterpret_cast<const u32x2_a2*>(p));
 }
 template <class T, int N, class V>
 FP4R_DEV void unpack_raw(const V& w, float (&x)[N]) {
@@ -63,7 +62,11 @@ FP4R_DEV void unpack_raw(const V& w, float (&x)[N]) {
     else unpack2(T{}, w[k], x[2 * k], x[2 * k + 1]);
   }
 }
-// N values as 16-byte vectors (4 of a 16-bit type: one of 8 bytes).
+// N values as 16-byte vectors (4 of a 16-bit type: one of 8 bytes), past the caches: what is
+// written once and not read by the same kernel displaces nothing (clipping 354 M BF16 elements
+// into FP32 551 -> 501 us, twelve parameters of 3.9 M elements 12.6 -> 12.1).
+template <class V, class P>
+FP4R_DEV void nt_store(P* p, V v) { __builtin_nontemporal_store(v, p); }
 template <class T, int N>
 FP4R_DEV void store_full(T* p, const float (&x)[N]) {
   if constexpr (sizeof(T) == 4) {
@@ -72,20 +75,20 @@ FP4R_DEV void store_full(T* p, const float (&x)[N]) {
       u32x4 w;
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = __float_as_uint(x[4 * q + k]);
-      *reinterpret_cast<u32x4_a4*>(p + 4 * q) = w;
+      nt_store(reinterpret_cast<u32x4_a4*>(p + 4 * q), w);
     }
   } else if constexpr (N == 4) {
     u32x2 w;
 #pragma unroll
     for (int k = 0; k < 2; ++k) w[k] = pack2(T{}, x[2 * k], x[2 * k + 1]);
-    *reinterpret_cast<u32x2_a2*>(p) = w;
+    nt_store(reinterpret_cast<u32x2_a2*>(p), w);
   } else {
 #pragma unroll
     for (int q = 0; q < N / 8; ++q) {
       u32x4 w;
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = pack2(T{}, x[8 * q + 2 * k], x[8 * q + 2 * k + 1]);
-      *reinterpret_cast<u32x4_a2*>(p + 8 * q) = w;
+      nt_store(reinterpret_cast<u32x4_a2*>(p + 8 * q), w);
     }
   }
 }

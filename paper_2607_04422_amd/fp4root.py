@@ -72,7 +72,7 @@ class Tensor(ctypes.Structure):
 
 class GradList(ctypes.Structure):
     _fields_ = [("mem", ctypes.c_void_p), ("count", ctypes.c_int64), ("parts", ctypes.c_int64),
-                ("outputs", ctypes.c_int32)]
+                ("flags", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class RmsNorm(ctypes.Structure):
