@@ -1626,6 +1626,12 @@ bool gain_ok(const void* gain, int32_t type) {
 }
 // Rows per launch: a grid of a workgroup of up to 1024 threads a row stays below 2^32 threads.
 constexpr int64_t kNormRows = int64_t(1) << 21;
+// The residual was written a layer ago and h is read a layer later, so both pass the caches; x
+// comes from the product before, which the 256 MB last-level cache still holds unless x takes
+// more than half of it.  8192 x 4096 BF16: nothing past them 47.2 us, h 44.6, both 39.5, x too
+// 41.3; with all of it in the cache beforehand 39.0, 40.9, 41.3, 42.7.  16384 x 8192, which does
+// not fit: 167, 164, 161, 152.
+constexpr int64_t kNormCached = int64_t(128) << 20;
 }  // namespace
 
 int fp4root_rmsnorm_quantize(const fp4root_rmsnorm* args, void* stream) {
@@ -1682,6 +1688,7 @@ int fp4root_rmsnorm_quantize(const fp4root_rmsnorm* args, void* stream) {
     k.type = a.type;
     k.gain_f32 = a.gain_type == FP4ROOT_FLOAT32;
     k.e8m0 = e8m0;
+    k.x_past = a.rows * a.cols * size > kNormCached;
     k.eps = a.eps;
     FP4R_TRY(launch_rmsnorm(k, (hipStream_t)stream));
   }

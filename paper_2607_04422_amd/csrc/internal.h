@@ -437,6 +437,7 @@ struct RmsArgs {
   int64_t rows, ld_x, ld_r, ld_h, ld_y;
   int32_t cols, group, groups;   // group: columns a scale covers, 0 for the row; groups: scales a row
   int32_t type, gain_f32, e8m0;
+  int32_t x_past;          // x is read past the caches
   double eps;
 };
 hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st);

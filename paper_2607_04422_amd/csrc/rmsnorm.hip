@@ -106,14 +106,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
-    h[i] = load_raw8((const T*)a.x + row * a.ld_x + c, n);
+    h[i] = a.x_past ? load_raw8<T, true>((const T*)a.x + row * a.ld_x + c, n)
+                    : load_raw8<T>((const T*)a.x + row * a.ld_x + c, n);
   }
   if (a.r) {
     Raw8<T> r[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
-      r[i] = load_raw8((const T*)a.r + row * a.ld_r + c, n);
+      r[i] = load_raw8<T, true>((const T*)a.r + row * a.ld_r + c, n);
     }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
-    if (a.h) store_raw8((T*)a.h + row * a.ld_h + c, n, h[i]);
+    if (a.h) store_raw8<T, true>((T*)a.h + row * a.ld_h + c, n, h[i]);
     float u[8];
     unpack8(h[i], u);
 #pragma unroll
@@ -237,9 +238,13 @@ void pick_rmsnorm(const RmsArgs& a, hipStream_t st) {
 // its columns' part of dgain in registers; at the end the slots are added in LDS and the
 // workgroup writes one row of partials, which k_rms_dgain adds in order.
 
+// Threads of a workgroup: 512, or a row's where it takes more (1024 threads for all widths:
+// 8192 x 2048 31.0 us for 29.0, 8192 x 4096 58.0 for 56.0).
+constexpr int bwd_threads(int tpr) { return tpr < 512 ? 512 : tpr; }
+
 template <class T, int TPR, int VPT>
-__global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_rms_bwd(RmsBwdArgs a) {
-  constexpr int NT = TPR < 512 ? 512 : TPR, RPG = NT / TPR, WPR = TPR / 64;
+__global__ __launch_bounds__(bwd_threads(TPR)) void k_rms_bwd(RmsBwdArgs a) {
+  constexpr int NT = bwd_threads(TPR), RPG = NT / TPR, WPR = TPR / 64;
   __shared__ float red[2][NT / 64];
   __shared__ float slab[RPG > 1 ? NT * 8 : 1];
   const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
@@ -253,11 +258,15 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_rms_bwd(RmsBwdArgs a)
   for (int64_t base = (int64_t)blockIdx.x * RPG; base < a.rows; base += (int64_t)gridDim.x * RPG, side ^= 1) {
     const int64_t row = base + slot;
     const bool live = row < a.rows;
+    // h was written in the forward pass, long ago; dy and dh were written just now, and dx is
+    // read soon: h passes the caches, and so does dx, which is written after all that is read
+    // (8192 x 4096 BF16: 57.0 us with nothing past them, 55.0 so, and 16384 x 8192: 197, 194;
+    // with dy and dh past them too, 2048 x 4096, which fit: 22.6 us for 19.6)
     Raw8<T> h[VPT], d[VPT], e[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int c = (i * TPR + t) * 8, n = live ? min(8, a.cols - c) : 0;
-      h[i] = load_raw8((const T*)a.h + row * a.ld_h + c, n);
+      h[i] = load_raw8<T, true>((const T*)a.h + row * a.ld_h + c, n);
       d[i] = load_raw8((const T*)a.dy + row * a.ld_dy + c, n);
     }
     if (a.dh) {
@@ -297,11 +306,10 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_rms_bwd(RmsBwdArgs a)
       for (int w = 1; w < WPR; ++w) dot += red[side][slot * WPR + w];
     }
     const float mean = dot * inv_cols;
-    if (!live) continue;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
-      if (n <= 0) continue;
+      if (!live || n <= 0) continue;
       float x[8], y[8], g[8], o[8];
       unpack8(h[i], x);
       unpack8(d[i], y);
@@ -318,7 +326,7 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_rms_bwd(RmsBwdArgs a)
 #pragma unroll
         for (int k = 0; k < 8; ++k) o[k] += x[k];
       }
-      store_raw8((T*)a.dx + row * a.ld_dx + c, n, pack8<T>(o));
+      store_raw8<T, true>((T*)a.dx + row * a.ld_dx + c, n, pack8<T>(o));
     }
   }
   if (!a.dgain) return;
@@ -341,27 +349,42 @@ __global__ __launch_bounds__(TPR < 512 ? 512 : TPR) void k_rms_bwd(RmsBwdArgs a)
   }
 }
 
-// 64 columns by 16 slices of the partial rows a workgroup.
-__global__ __launch_bounds__(1024) void k_rms_dgain(const float* partial, int64_t count, int cols, float* dgain) {
-  __shared__ float red[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
-  float s = 0.0f;
-  if (c < cols)
-    for (int64_t p = slice; p < count; p += 16) s += partial[p * cols + c];
-  red[slice][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (slice == 0 && c < cols) {
+// 16 columns by 64 slices of the partial rows a workgroup: each thread adds four columns of
+// every 64th row, eight loads in flight, then the slices in pairs.
+__global__ __launch_bounds__(256) void k_rms_dgain(const float* partial, int count, int cols, float* dgain) {
+  __shared__ float red[16][65];
+  const int q = threadIdx.x & 3, slice = threadIdx.x >> 2, c = blockIdx.x * 16 + q * 4, n = min(4, cols - c);
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (n > 0) {
+    for (int p = slice; p < count; p += 64 * 8) {
+      float x[8][4];
 #pragma unroll
-    for (int q = 1; q < 16; ++q) s += red[q][threadIdx.x & 63];
-    dgain[c] = s;
+      for (int u = 0; u < 8; ++u) load_vec<float, 4>(partial + (int64_t)min(p + u * 64, count - 1) * cols + c, n, x[u]);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] += p + u * 64 < count ? x[u][k] : 0.0f;
+    }
   }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) red[q * 4 + k][slice] = s[k];
+  __syncthreads();
+  // 16 threads a column
+  const int col = threadIdx.x >> 4, l = threadIdx.x & 15;
+  float v = (red[col][l] + red[col][l + 16]) + (red[col][l + 32] + red[col][l + 48]);
+#pragma unroll
+  for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o);
+  if (l == 0 && blockIdx.x * 16 + col < cols) dgain[blockIdx.x * 16 + col] = v;
 }
 
+// Threads and vectors a row.  A thread keeps 8 columns where 512 threads cover the row, so that
+// 4 to 6 waves fit a SIMD (16384 x 8192: 2 vectors of 512 threads 197 us, 4 of 256 222, 1 of
+// 1024 209; 8192 x 4096: 1 of 512 56.0, 2 of 256 56.8, 4 of 128 66.8).
 struct BwdShape {
   int tpr, vpt;
 };
 BwdShape bwd_shape(int64_t cols) {
-  const int tpr = cols <= 1024 ? 64 : cols <= 8192 ? 256 : 1024;
+  const int tpr = cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 8192 ? 512 : 1024;
   const int64_t v = (cols + 8 * tpr - 1) / (8 * tpr);
   return {tpr, v <= 1 ? 1 : v <= 2 ? 2 : 4};
 }
@@ -369,17 +392,17 @@ BwdShape bwd_shape(int64_t cols) {
 template <class T>
 void run_bwd(const RmsBwdArgs& a, uint32_t grid, hipStream_t st) {
   const BwdShape s = bwd_shape(a.cols);
-  const dim3 nt(s.tpr < 512 ? 512 : s.tpr);
+  const dim3 nt(bwd_threads(s.tpr));
 #define FP4R_BWD(TPR, VPT)                                                              \
   if (s.tpr == TPR && s.vpt == VPT) {                                                   \
     hipLaunchKernelGGL((k_rms_bwd<T, TPR, VPT>), dim3(grid), nt, 0, st, a);             \
     return;                                                                             \
   }
   FP4R_BWD(64, 1)
-  FP4R_BWD(64, 2)
+  FP4R_BWD(128, 1)
   FP4R_BWD(256, 1)
-  FP4R_BWD(256, 2)
-  FP4R_BWD(256, 4)
+  FP4R_BWD(512, 1)
+  FP4R_BWD(512, 2)
   FP4R_BWD(1024, 2)
   FP4R_BWD(1024, 4)
 #undef FP4R_BWD
@@ -396,10 +419,12 @@ hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Two workgroups of 512 threads a CU, or one of 1024: each more adds a row of partials (8192 x
+// 4096: 256 workgroups 62.8 us, 512 56.1, 768 56.0, 1024 63.3).
 int64_t rms_bwd_groups(int64_t rows, int64_t cols) {
-  const int tpr = bwd_shape(cols).tpr, slots = tpr < 512 ? 512 / tpr : 1;
-  const int64_t all = (rows + slots - 1) / slots;
-  return all < 512 ? all : 512;
+  const int tpr = bwd_shape(cols).tpr, slots = bwd_threads(tpr) / tpr;
+  const int64_t all = (rows + slots - 1) / slots, most = bwd_threads(tpr) == 512 ? 512 : 256;
+  return all < most ? all : most;
 }
 
 hipError_t launch_rmsnorm_backward(const RmsBwdArgs& a, hipStream_t st) {
@@ -412,7 +437,7 @@ hipError_t launch_rmsnorm_backward(const RmsBwdArgs& a, hipStream_t st) {
     }
   }
   if (a.dgain)
-    hipLaunchKernelGGL(k_rms_dgain, dim3((uint32_t)((a.cols + 63) / 64)), dim3(1024), 0, st, a.partial, (int64_t)grid,
+    hipLaunchKernelGGL(k_rms_dgain, dim3((uint32_t)((a.cols + 15) / 16)), dim3(256), 0, st, a.partial, (int)grid,
                        (int)a.cols, a.dgain);
   return hipGetLastError();
 }

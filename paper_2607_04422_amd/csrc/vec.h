@@ -47,6 +47,11 @@ FP4R_DEV V load_as(const P* p) {
   if constexpr (NT) return __builtin_nontemporal_load(p);
   else return *p;
 }
+template <bool NT, class V, class P>
+FP4R_DEV void store_as(P* p, V v) {
+  if constexpr (NT) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
 template <class T, int N, bool NT = false>
 FP4R_DEV auto load_raw(const T* p) {
   static_assert(N * sizeof(T) == 16 || (N * sizeof(T) == 8 && sizeof(T) == 2), "one vector");
@@ -65,8 +70,6 @@ FP4R_DEV void unpack_raw(const V& w, float (&x)[N]) {
 // N values as 16-byte vectors (4 of a 16-bit type: one of 8 bytes), past the caches: what is
 // written once and not read by the same kernel displaces nothing (clipping 354 M BF16 elements
 // into FP32 551 -> 501 us, twelve parameters of 3.9 M elements 12.6 -> 12.1).
-template <class V, class P>
-FP4R_DEV void nt_store(P* p, V v) { __builtin_nontemporal_store(v, p); }
 template <class T, int N>
 FP4R_DEV void store_full(T* p, const float (&x)[N]) {
   if constexpr (sizeof(T) == 4) {
@@ -75,20 +78,20 @@ FP4R_DEV void store_full(T* p, const float (&x)[N]) {
       u32x4 w;
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = __float_as_uint(x[4 * q + k]);
-      nt_store(reinterpret_cast<u32x4_a4*>(p + 4 * q), w);
+      store_as<true>(reinterpret_cast<u32x4_a4*>(p + 4 * q), w);
     }
   } else if constexpr (N == 4) {
     u32x2 w;
 #pragma unroll
     for (int k = 0; k < 2; ++k) w[k] = pack2(T{}, x[2 * k], x[2 * k + 1]);
-    nt_store(reinterpret_cast<u32x2_a2*>(p), w);
+    store_as<true>(reinterpret_cast<u32x2_a2*>(p), w);
   } else {
 #pragma unroll
     for (int q = 0; q < N / 8; ++q) {
       u32x4 w;
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = pack2(T{}, x[8 * q + 2 * k], x[8 * q + 2 * k + 1]);
-      nt_store(reinterpret_cast<u32x4_a2*>(p + 8 * q), w);
+      store_as<true>(reinterpret_cast<u32x4_a2*>(p + 8 * q), w);
     }
   }
 }
@@ -123,15 +126,15 @@ template <class T>
 struct Raw8 {
   uint32_t w[2 * sizeof(T)];
 };
-template <class T>
+template <class T, bool NT = false>
 FP4R_DEV Raw8<T> load_raw8(const T* p, int n) {
   Raw8<T> r;
   if (n >= 8) {
 #pragma unroll
     for (int q = 0; q < (int)sizeof(T) / 2; ++q) {
       u32x4 v;
-      if constexpr (sizeof(T) == 4) v = *reinterpret_cast<const u32x4_a4*>(p + 4 * q);
-      else v = *reinterpret_cast<const u32x4_a2*>(p);
+      if constexpr (sizeof(T) == 4) v = load_as<NT, u32x4>(reinterpret_cast<const u32x4_a4*>(p + 4 * q));
+      else v = load_as<NT, u32x4>(reinterpret_cast<const u32x4_a2*>(p));
 #pragma unroll
       for (int k = 0; k < 4; ++k) r.w[4 * q + k] = v[k];
     }
@@ -148,7 +151,7 @@ FP4R_DEV Raw8<T> load_raw8(const T* p, int n) {
   }
   return r;
 }
-template <class T>
+template <class T, bool NT = false>
 FP4R_DEV void store_raw8(T* p, int n, const Raw8<T>& r) {
   if (n >= 8) {
 #pragma unroll
@@ -156,8 +159,8 @@ FP4R_DEV void store_raw8(T* p, int n, const Raw8<T>& r) {
       u32x4 v;
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = r.w[4 * q + k];
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_a4*>(p + 4 * q) = v;
-      else *reinterpret_cast<u32x4_a2*>(p) = v;
+      if constexpr (sizeof(T) == 4) store_as<NT>(reinterpret_cast<u32x4_a4*>(p + 4 * q), v);
+      else store_as<NT>(reinterpret_cast<u32x4_a2*>(p), v);
     }
   } else {
 #pragma unroll
