@@ -22,26 +22,29 @@ constexpr float kAmaxMin = 0x1p-100f;
 
 // Lanes l and l ^ 1, l ^ 2 of a quad, then the other quad of 8 lanes, the other half of 16.
 template <int CTRL>
-FP4R_DEV float dpp_max(float v) {
-  return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, true)));
+FP4R_DEV float dpp_f(float v) {
+  return __uint_as_float(dpp_u<CTRL>(__float_as_uint(v)));
 }
 FP4R_DEV float group_max(float v, int lanes) {   // lanes: 4, 8 or 16 (uniform)
-  v = dpp_max<0xB1>(v);
-  v = dpp_max<0x4E>(v);
-  if (lanes > 4) v = dpp_max<0x141>(v);
-  if (lanes > 8) v = dpp_max<0x140>(v);
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  if (lanes > 4) v = fmaxf(v, dpp_f<0x141>(v));
+  if (lanes > 8) v = fmaxf(v, dpp_f<0x140>(v));
   return v;
 }
-
-FP4R_DEV double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+FP4R_DEV float lane_f(float v, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+FP4R_DEV float wave_max(float v) {
+  v = group_max(v, 16);
+  return fmaxf(fmaxf(lane_f(v, 0), lane_f(v, 16)), fmaxf(lane_f(v, 32), lane_f(v, 48)));
 }
 FP4R_DEV float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  v = v + dpp_f<0xB1>(v);
+  v = v + dpp_f<0x4E>(v);
+  v = v + dpp_f<0x141>(v);
+  v = v + dpp_f<0x140>(v);
+  return (lane_f(v, 0) + lane_f(v, 16)) + (lane_f(v, 32) + lane_f(v, 48));
 }
 
 // 1 / sqrt(a) for 0 < a < 2^1000: the instruction's estimate and two Newton steps.
@@ -72,9 +75,28 @@ FP4R_DEV void store_scale(const RmsArgs& a, int64_t i, uint32_t stored) {
   else reinterpret_cast<uint32_t*>(a.scales)[i] = stored;
 }
 
-FP4R_DEV void load_gain(const void* gain, int f32, int col, int n, float (&g)[8]) {
-  if (f32) unpack8(load_raw8((const float*)gain + col, n), g);
-  else unpack8(load_raw8((const bf16_t*)gain + col, n), g);
+// Eight gains as they lie in memory: words of FP32, or half as many of BF16.
+struct Gain8 {
+  Raw8<float> f;
+};
+FP4R_DEV Gain8 load_gain(const void* gain, int f32, int col, int n) {
+  Gain8 g;
+  if (f32) {
+    g.f = load_raw8((const float*)gain + col, n);
+  } else {
+    const Raw8<bf16_t> b = load_raw8((const bf16_t*)gain + col, n);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g.f.w[k] = b.w[k];
+  }
+  return g;
+}
+FP4R_DEV void unpack_gain(const Gain8& g, int f32, float (&x)[8]) {
+  if (f32) {
+    unpack8(g.f, x);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) unpack2(bf16_t{}, g.f.w[k], x[2 * k], x[2 * k + 1]);
+  }
 }
 
 FP4R_DEV void store_codes(uint8_t* p, int n, const float (&y)[8], float inv) {
@@ -97,15 +119,16 @@ template <class T, int TPR, int VPT>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
   constexpr int WPR = TPR / 64;                       // waves a row
   constexpr int RPG = TPR < 256 ? 256 / TPR : 1;      // rows a workgroup
-  __shared__ double red_s[WPR];
-  __shared__ float red_m[WPR];
-  const int64_t row = (int64_t)blockIdx.x * RPG + threadIdx.x / TPR;
-  const int t = threadIdx.x % TPR;
-  if (RPG > 1 && row >= a.rows) return;               // whole waves, and no barrier follows
+  __shared__ double red_s[RPG][WPR];
+  __shared__ float red_m[RPG][WPR];
+  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const int64_t row = (int64_t)blockIdx.x * RPG + slot;
+  const bool live = RPG == 1 || row < a.rows;
+  const int cols = live ? a.cols : 0;                 // a slot past the last row reads and writes nothing
   Raw8<T> h[VPT];
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    const int c = (i * TPR + t) * 8, n = min(8, cols - c);
     h[i] = a.x_past ? load_raw8<T, true>((const T*)a.x + row * a.ld_x + c, n)
                     : load_raw8<T>((const T*)a.x + row * a.ld_x + c, n);
   }
@@ -113,7 +136,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
     Raw8<T> r[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+      const int c = (i * TPR + t) * 8, n = min(8, cols - c);
       r[i] = load_raw8<T, true>((const T*)a.r + row * a.ld_r + c, n);
     }
 #pragma unroll
@@ -126,45 +149,56 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
       h[i] = pack8<T>(u);
     }
   }
+  // the gain is on its way while the row is summed
+  Gain8 gain[VPT];
+  if (a.gain) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int c = (i * TPR + t) * 8;
+      gain[i] = load_gain(a.gain, a.gain_f32, c, min(8, cols - c));
+    }
+  }
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    const int c = (i * TPR + t) * 8, n = min(8, cols - c);
     if (a.h) store_raw8<T, true>((T*)a.h + row * a.ld_h + c, n, h[i]);
     float u[8];
     unpack8(h[i], u);
 #pragma unroll
     for (int k = 0; k < 8; ++k) s = __builtin_fma((double)u[k], (double)u[k], s);
   }
-  s = wave_sum(s);
+  s = wave_sum_d(s);
   if constexpr (WPR > 1) {
-    if ((threadIdx.x & 63) == 0) red_s[threadIdx.x >> 6] = s;
+    if ((t & 63) == 0) red_s[slot][t >> 6] = s;
     __syncthreads();
-    s = red_s[0];
+    s = red_s[slot][0];
 #pragma unroll
-    for (int w = 1; w < WPR; ++w) s += red_s[w];
+    for (int w = 1; w < WPR; ++w) s += red_s[slot][w];
   }
   const float rstd = (float)rsqrt64(s / (double)a.cols + a.eps);
-  if (t == 0) {
+  if (t == 0 && live) {
     if (a.rstd) a.rstd[row] = rstd;
     if (a.status && !(s < __builtin_inf())) *a.status = kErrNonFinite;
   }
   if (!a.codes && !a.y) return;
+  const auto normalised = [&](int i, float (&y)[8]) {
+    unpack8(h[i], y);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] *= rstd;
+    if (!a.gain) return;
+    float g[8];
+    unpack_gain(gain[i], a.gain_f32, g);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] *= g[k];
+  };
   float top = 0.0f;
   const int lanes = a.group / 8;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
-    float y[8], g[8];
-    unpack8(h[i], y);
-    if (a.gain) {
-      load_gain(a.gain, a.gain_f32, c, n, g);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = (y[k] * rstd) * g[k];
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] *= rstd;
-    }
+    const int c = (i * TPR + t) * 8, n = min(8, cols - c);
+    float y[8];
+    normalised(i, y);
     if (a.y) store_raw8((T*)a.y + row * a.ld_y + c, n, pack8<T>(y));
     if (!a.codes) continue;
     float m = 0.0f;
@@ -183,35 +217,26 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
     top = fmaxf(top, m);
   }
   if (!a.codes || lanes) return;
-#pragma unroll
-  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  top = wave_max(top);
   if constexpr (WPR > 1) {
-    if ((threadIdx.x & 63) == 0) red_m[threadIdx.x >> 6] = top;
+    if ((t & 63) == 0) red_m[slot][t >> 6] = top;
     __syncthreads();
-    top = red_m[0];
+    top = red_m[slot][0];
 #pragma unroll
-    for (int w = 1; w < WPR; ++w) top = fmaxf(top, red_m[w]);
+    for (int w = 1; w < WPR; ++w) top = fmaxf(top, red_m[slot][w]);
   }
   uint32_t stored;
   const float inv = scale_of(top, a.e8m0, stored);
-  if (t == 0) {
+  if (t == 0 && live) {
     store_scale(a, row, stored);
     if (a.status && !(top < __builtin_inff())) *a.status = kErrNonFinite;
   }
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
+    const int c = (i * TPR + t) * 8, n = min(8, cols - c);
     if (n <= 0) continue;
-    float y[8], g[8];
-    unpack8(h[i], y);
-    if (a.gain) {
-      load_gain(a.gain, a.gain_f32, c, n, g);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = (y[k] * rstd) * g[k];
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] *= rstd;
-    }
+    float y[8];
+    normalised(i, y);
     store_codes(a.codes + row * a.cols + c, n, y, inv);
   }
 }
@@ -222,13 +247,22 @@ void run_rmsnorm(const RmsArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_rmsnorm<T, TPR, VPT>), dim3((uint32_t)((a.rows + RPG - 1) / RPG)), dim3(NT), 0, st, a);
 }
 
+// Many rows: 8 or 16 columns a thread (8192 x 4096: 2 vectors of 256 threads 42.3 us, 1 of 512
+// 44.0, 4 of 128 44.4, 8 of 64 49.5; 16384 x 8192: 2 of 512 160, 4 of 256 161, 1 of 1024 188).
+// Few rows do not fill the CUs, so that a row's own latency counts: as many threads as its
+// columns allow (1 x 4096: 1 of 512 3.5 us, 2 of 256 4.2, 8 of 64 8.7; 256 rows 3.9, 4.6, 10.0;
+// 1024 rows 8.3, 7.4, 11.7).
+constexpr int64_t kFewRows = 512;
 template <class T>
 void pick_rmsnorm(const RmsArgs& a, hipStream_t st) {
+  const bool few = a.rows <= kFewRows;
   if (a.cols <= 512) run_rmsnorm<T, 64, 1>(a, st);
-  else if (a.cols <= 1024) run_rmsnorm<T, 64, 2>(a, st);
+  else if (a.cols <= 1024) run_rmsnorm<T, 128, 1>(a, st);
   else if (a.cols <= 2048) run_rmsnorm<T, 256, 1>(a, st);
+  else if (a.cols <= 4096 && few) run_rmsnorm<T, 512, 1>(a, st);
   else if (a.cols <= 4096) run_rmsnorm<T, 256, 2>(a, st);
-  else if (a.cols <= 8192) run_rmsnorm<T, 256, 4>(a, st);
+  else if (a.cols <= 8192 && few) run_rmsnorm<T, 1024, 1>(a, st);
+  else if (a.cols <= 8192) run_rmsnorm<T, 512, 2>(a, st);
   else if (a.cols <= 16384) run_rmsnorm<T, 1024, 2>(a, st);
   else run_rmsnorm<T, 1024, 4>(a, st);
 }
@@ -285,7 +319,7 @@ __global__ __launch_bounds__(bwd_threads(TPR)) void k_rms_bwd(RmsBwdArgs a) {
       unpack8(h[i], x);
       unpack8(d[i], y);
       if (a.gain) {
-        load_gain(a.gain, a.gain_f32, c, n, g);
+        unpack_gain(load_gain(a.gain, a.gain_f32, c, n), a.gain_f32, g);
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) g[k] = 1.0f;
@@ -314,7 +348,7 @@ __global__ __launch_bounds__(bwd_threads(TPR)) void k_rms_bwd(RmsBwdArgs a) {
       unpack8(h[i], x);
       unpack8(d[i], y);
       if (a.gain) {
-        load_gain(a.gain, a.gain_f32, c, n, g);
+        unpack_gain(load_gain(a.gain, a.gain_f32, c, n), a.gain_f32, g);
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) g[k] = 1.0f;
