@@ -436,7 +436,7 @@ typedef struct {
   int32_t group;         /* columns a scale covers: 32, 64 or 128 (the last group of a row may
                             be shorter), or 0: the row                                        */
   int32_t scale_type;    /* FP4ROOT_SCALE_*                                                   */
-  double eps;            /* > 0, finite                                                       */
+  double eps;            /* >= 2^-126, finite                                                 */
 } fp4root_rmsnorm;
 
 /* h = round(x + residual) (x without a residual), rstd = fl32(1 / sqrt(sum h^2 / cols + eps))
@@ -453,7 +453,8 @@ size_t fp4root_rmsnorm_backward_workspace(int64_t rows, int64_t cols);
  *   g = dy gain, xhat = h rstd, dx = rstd (g - xhat mean(g xhat)) + dh,
  *   dgain = sum over rows of dy xhat.
  * dx is the gradient of x and of the residual alike, rounded once; dgain is FP32 (what
- * fp4root_qadamw_update reads) and its sum's order depends on the shape alone.
+ * fp4root_qadamw_update reads) and its sum's order depends on the shape alone.  A row whose rstd
+ * is NaN has a dx of NaN, and makes dgain NaN.
  *   dy, h, dh (gradient that reaches h past the norm, or NULL), dx: rows x cols of `type`, row
  *   strides ld_*; dx may be dy, h or dh; rstd: rows floats; gain: cols, or NULL for ones;
  *   dgain: cols floats, or NULL (then ws may be NULL).  cols in [1, 32768]. */

@@ -1640,7 +1640,8 @@ int fp4root_rmsnorm_quantize(const fp4root_rmsnorm* args, void* stream) {
   if (!type_ok(a.type) || !gain_ok(a.gain, a.gain_type)) return FP4ROOT_ERR_INVALID_ARG;
   if (a.group != 0 && a.group != 32 && a.group != 64 && a.group != 128) return FP4ROOT_ERR_INVALID_ARG;
   if (a.scale_type != FP4ROOT_SCALE_FP32 && a.scale_type != FP4ROOT_SCALE_E8M0) return FP4ROOT_ERR_INVALID_ARG;
-  if (!(a.eps > 0.0) || !std::isfinite(a.eps)) return FP4ROOT_ERR_INVALID_ARG;
+  // below, a row of zeros would have an infinite rstd
+  if (!(a.eps >= 0x1p-126) || !std::isfinite(a.eps)) return FP4ROOT_ERR_INVALID_ARG;
   if (!norm_shape_ok(a.rows, a.cols)) return FP4ROOT_ERR_SHAPE;
   if (a.rows == 0) return FP4ROOT_OK;
   const int64_t size = type_size(a.type), groups = a.group ? (a.cols + a.group - 1) / a.group : 1;

@@ -453,11 +453,13 @@ hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Two workgroups of 512 threads a CU, or one of 1024: each more adds a row of partials (8192 x
-// 4096: 256 workgroups 62.8 us, 512 56.1, 768 56.0, 1024 63.3).
+// One workgroup a CU, or two of 512 threads where each then has four turns at least: every one
+// adds a row of partials (256 and 512 workgroups: 1024 x 4096 14.9 and 17.1 us, 2048 x 4096 20.1
+// and 19.9, 4096 x 4096 32.8 and 30.4, 32768 x 128 38.5 and 25.5; 2048 x 16384, of 1024 threads,
+// 63.7 and 72.0).
 int64_t rms_bwd_groups(int64_t rows, int64_t cols) {
   const int tpr = bwd_shape(cols).tpr, slots = bwd_threads(tpr) / tpr;
-  const int64_t all = (rows + slots - 1) / slots, most = bwd_threads(tpr) == 512 ? 512 : 256;
+  const int64_t all = (rows + slots - 1) / slots, most = bwd_threads(tpr) == 512 && all >= 2048 ? 512 : 256;
   return all < most ? all : most;
 }
 

@@ -62,6 +62,7 @@ FLOAT32, BFLOAT16, FLOAT16 = 0, 1, 2
 NORM_L2, NORM_MAX = 0, 1
 SCALE_FP32, SCALE_E8M0 = 0, 1
 _TYPES = {torch.float32: FLOAT32, torch.bfloat16: BFLOAT16, torch.float16: FLOAT16}
+_GAIN_TYPES = {torch.float32: FLOAT32, torch.bfloat16: BFLOAT16}
 
 
 class Tensor(ctypes.Structure):
@@ -693,10 +694,11 @@ def _matrix(t: torch.Tensor, name: str, like: torch.Tensor = None):
     rows of one stride; checked against `like` for type, shape and GPU."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if like is not None and (t.dtype != like.dtype or t.shape != like.shape or t.device != like.device):
+    shape = t.shape
+    if like is not None and (t.dtype is not like.dtype or shape != like.shape or t.device != like.device):
         raise TypeError(f"{name} must have x's type, shape and GPU")
+    cols = shape[-1]
     if t.is_contiguous():
-        cols = t.shape[-1]
         return (t.numel() // cols if cols else 0), cols
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} rows must be contiguous")
@@ -716,22 +718,24 @@ def _matrix(t: torch.Tensor, name: str, like: torch.Tensor = None):
 def _gain_type(gain, x):
     if gain is None:
         return FLOAT32
-    if not isinstance(gain, torch.Tensor) or not gain.is_cuda or gain.device != x.device or \
-            gain.dtype not in (torch.float32, torch.bfloat16):
+    if not isinstance(gain, torch.Tensor) or gain.device != x.device or gain.dtype not in _GAIN_TYPES:
         raise TypeError("gain must be a float32 or bfloat16 tensor on x's GPU")
     if gain.dim() != 1 or gain.shape[0] != x.shape[-1] or not gain.is_contiguous():
         raise ValueError("gain must be a contiguous vector of x's columns")
-    return _TYPES[gain.dtype]
+    return _GAIN_TYPES[gain.dtype]
 
 
-def _need_stream(x, name: str):
-    load()
+def _need_stream(x, name: str) -> int:
+    """The type of a matrix that a norm reads, checked."""
+    if _lib is None:
+        load()
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if x.dtype not in _TYPES:
         raise TypeError(f"{name} must be float32, bfloat16 or float16")
     if x.dim() < 1:
         raise ValueError(f"{name} must have a dimension of columns")
+    return _TYPES[x.dtype]
 
 
 def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residual: torch.Tensor = None,
@@ -743,7 +747,7 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     float16, rows of one stride; out: an earlier call's result, whose tensors are written again
     (h may be the residual or x itself: in place); status: an int32 GPU tensor of one element.
     See fp4root_rmsnorm_quantize in include/fp4root.h."""
-    _need_stream(x, "x")
+    type_ = _need_stream(x, "x")
     gain_type = _gain_type(gain, x)
     rows, ld_x = _matrix(x, "x")
     shape, dev = x.shape, x.device
@@ -752,12 +756,14 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     raw = _launch_stream(dev, stream)
     if out is None:
         codes = scales = y = None
-        packed = x.is_contiguous()         # empty_like keeps a stride, and is the cheaper call
+        # empty_like keeps a stride, and is the cheaper call
+        packed = ld_x == cols and x.is_contiguous()
         if quantize:
             codes = torch.empty_like(x, dtype=torch.uint8) if packed else x.new_empty(shape, dtype=torch.uint8)
             scales = x.new_empty((*lead, -(-cols // group)) if group > 0 else lead,
                                  dtype=torch.uint8 if e8m0 else torch.float32)
-        rstd = x.new_empty(lead, dtype=torch.float32)
+        rstd = torch.empty_like(scales) if quantize and group == 0 and not e8m0 else \
+            x.new_empty(lead, dtype=torch.float32)
         h = x if residual is None else torch.empty_like(x) if packed else x.new_empty(shape)
         if want_y:
             y = x.new_empty(shape)
@@ -786,7 +792,7 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
                 h.data_ptr() if residual is not None and h is not None else None,
                 y.data_ptr() if y is not None else None, codes.data_ptr() if codes is not None else None,
                 scales.data_ptr() if scales is not None else None, rstd.data_ptr() if rstd is not None else None,
-                status.data_ptr() if status is not None else None, rows, cols, ld_x, ld_r, ld_h, ld_y, _TYPES[x.dtype],
+                status.data_ptr() if status is not None else None, rows, cols, ld_x, ld_r, ld_h, ld_y, type_,
                 gain_type, group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps)
     _check(_call(_lib.fp4root_rmsnorm_quantize, dev, ctypes.byref(a), raw), "fp4root_rmsnorm_quantize")
     return out
@@ -798,7 +804,7 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     """(dx, dgain) of the norm of h under the gradient dy of its output and dh of h itself; dx in
     h's type is the gradient of x and of the residual alike, dgain is float32.  dx may be given
     (dy, h or dh itself: in place); see fp4root_rmsnorm_backward in include/fp4root.h."""
-    _need_stream(h, "h")
+    type_ = _need_stream(h, "h")
     rows, ld_h = _matrix(h, "h")
     ld_dy = _matrix(dy, "dy", h)[1]
     ld_dh = _matrix(dh, "dh", h)[1] if dh is not None else 0
@@ -810,7 +816,7 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     raw = _launch_stream(dev, stream)
     new = []
     if dx is None:
-        dx = torch.empty_like(h) if h.is_contiguous() else h.new_empty(h.shape)
+        dx = torch.empty_like(h) if ld_h == cols and h.is_contiguous() else h.new_empty(h.shape)
         ld_dx = cols
         new.append(dx)
     else:
@@ -835,7 +841,7 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     _check(_call(_lib.fp4root_rmsnorm_backward, dev, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h,
                  dh.data_ptr() if dh is not None else None, ld_dh, gain.data_ptr() if gain is not None else None,
                  rstd.data_ptr(), dx.data_ptr(), ld_dx, dgain.data_ptr() if dgain is not None else None, rows, cols,
-                 _TYPES[h.dtype], gain_type, ws.data_ptr() if need else None,
+                 type_, gain_type, ws.data_ptr() if need else None,
                  ws.numel() * ws.element_size() if need else 0, raw), "fp4root_rmsnorm_backward")
     return dx, dgain
 

@@ -116,7 +116,7 @@ def rms(**kw):
 def test_rmsnorm_refusals():
     assert F.load().fp4root_rmsnorm_quantize(None, None) == -1
     for kw in (dict(type=3), dict(gain_type=2), dict(group=16), dict(group=-1), dict(scale_type=2), dict(eps=0.0),
-               dict(eps=NAN), dict(eps=INF), dict(x=None), dict(scales=None), dict(codes=None),
+               dict(eps=1e-39), dict(eps=NAN), dict(eps=INF), dict(x=None), dict(scales=None), dict(codes=None),
                dict(codes=None, scales=None), dict(x=P + 1), dict(gain=P + 1), dict(rstd=Q + 0x90001),
                dict(scales=Q + 0x80002), dict(status=Q + 0x90002)):
         assert rms(**kw) == -1, kw
