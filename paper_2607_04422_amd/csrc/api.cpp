@@ -1505,7 +1505,6 @@ size_t carve_grad_list(void* base, int64_t count, int64_t parts, GradTable& w) {
   w.status = cv.take<uint32_t>(1);
   w.tensors = cv.take<GradRef>((size_t)count + 1);
   w.parts = cv.take<GradPart>((size_t)parts);
-  w.sums = cv.take<double>((size_t)count);
   w.partial = cv.take<double>((size_t)parts);
   return cv.off;
 }

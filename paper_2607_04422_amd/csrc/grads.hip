@@ -143,83 +143,47 @@ FP4R_DEV void write_result(double total, bool max, double max_norm, double eps, 
   result[1] = q > 1.0 ? 1.0f : (float)q;   // a NaN stays
 }
 
-// Each tensor's parts (at most 1024), joined by a wave: lane l takes parts l, l + 64, ..., then
-// the lanes pairwise.  COUNT tensors at once with all their loads in flight (an index past the
-// end reads the last part and is dropped, since a branch would wait for each load).
-template <bool MAX, int COUNT>
-FP4R_DEV void join_tensors(const GradTable& tb, uint32_t count, uint32_t t0, uint32_t step, float* norms,
-                           double (&v)[COUNT]) {
-  const uint32_t lane = threadIdx.x & 63;
-  uint32_t at[COUNT], end[COUNT], most = 0;
+// Parts first, first + step, ... before end, U loads in flight (an index past the end reads the
+// last part and is dropped, since a branch would wait for each load).
+template <bool MAX, int U>
+FP4R_DEV double join_parts(const double* partial, uint32_t first, uint32_t step, uint32_t end) {
+  double v = 0.0;
+  for (uint32_t p = first; p < end; p += U * step) {
+    double x[U];
 #pragma unroll
-  for (int q = 0; q < COUNT; ++q) {
-    const uint32_t t = min(t0 + q * step, count - 1);
-    at[q] = tb.tensors[t].first;
-    end[q] = tb.tensors[t + 1].first;   // a tensor has a part at least
-    most = max(most, end[q] - at[q]);
-    v[q] = 0.0;
+    for (int u = 0; u < U; ++u) x[u] = partial[min(p + u * step, end - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v = join<MAX>(v, p + u * step < end ? x[u] : 0.0);
   }
-  constexpr int U = COUNT > 1 ? 1 : 4;
-  for (uint32_t p = 0; p < most; p += U * 64) {
-    double x[COUNT][U];
-#pragma unroll
-    for (int q = 0; q < COUNT; ++q)
-#pragma unroll
-      for (int u = 0; u < U; ++u) x[q][u] = tb.partial[min(at[q] + p + u * 64 + lane, end[q] - 1)];
-#pragma unroll
-    for (int q = 0; q < COUNT; ++q)
-#pragma unroll
-      for (int u = 0; u < U; ++u) v[q] = join<MAX>(v[q], at[q] + p + u * 64 + lane < end[q] ? x[q][u] : 0.0);
-  }
-#pragma unroll
-  for (int q = 0; q < COUNT; ++q) {
-    v[q] = wave_join<MAX>(v[q]);
-    if (t0 + q * step >= count) v[q] = 0.0;
-  }
-  // a lane for each tensor's root, which is a long chain of binary64 instructions
-  double mine = v[0];
-#pragma unroll
-  for (int q = 1; q < COUNT; ++q) mine = (int)lane == q ? v[q] : mine;
-  const uint32_t t = t0 + lane * step;
-  if (norms && lane < COUNT && t < count) norms[t] = (float)(MAX ? mine : __builtin_sqrt(mine));
+  return v;
 }
 
-template <bool MAX>
-__global__ __launch_bounds__(kThreads) void k_grad_tensors(GradTable tb, uint32_t count, float* norms) {
-  const uint32_t t = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  if (t >= count) return;
-  double v[1];
-  join_tensors<MAX, 1>(tb, count, t, 0, norms, v);
-  if ((threadIdx.x & 63) == 0) tb.sums[t] = v[0];
-}
-
-// The whole list, in one workgroup.  Short lists (kFused tensors of kFusedParts parts at most) it
-// joins from their parts; longer ones come joined by k_grad_tensors.
+// Workgroup 0 joins all parts into the total; the others, a wave a tensor, each tensor's own.
+// Neither waits for the other (300 tensors of 3400 parts, joined one after the other: 9.3 us in
+// two launches).
 constexpr int kWaves = 16;
-constexpr uint32_t kFused = kWaves * 4, kFusedParts = 2048;
 template <bool MAX>
-__global__ __launch_bounds__(kWaves * 64) void k_grad_total(GradTable tb, uint32_t count, int fused, double max_norm, double eps,
-                                                            double* total, float* norms, float* result) {
+__global__ __launch_bounds__(kWaves * 64) void k_grad_total(GradTable tb, uint32_t count, uint32_t parts,
+                                                            double max_norm, double eps, double* total, float* norms,
+                                                            float* result) {
   __shared__ double red[kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double all = 0.0;
-  if (!fused) {
-    for (uint32_t i = threadIdx.x; i < count; i += kWaves * 64) all = join<MAX>(all, tb.sums[i]);
-    all = wave_join<MAX>(all);
-  } else if (count > 0) {
-    double v[kFused / kWaves];
-    join_tensors<MAX, kFused / kWaves>(tb, count, wave, kWaves, norms, v);
-#pragma unroll
-    for (int q = 0; q < kFused / kWaves; ++q) all = join<MAX>(all, v[q]);
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (blockIdx.x > 0) {
+    const uint32_t t = (blockIdx.x - 1) * kWaves + wave;
+    if (t >= count) return;
+    const double v = wave_join<MAX>(join_parts<MAX, 4>(tb.partial, tb.tensors[t].first + lane, 64, tb.tensors[t + 1].first));
+    if (lane == 0) norms[t] = (float)(MAX ? v : __builtin_sqrt(v));
+    return;
   }
-  if (lane == 0) red[wave] = all;
+  double v = wave_join<MAX>(join_parts<MAX, 8>(tb.partial, threadIdx.x, kWaves * 64, parts));
+  if (lane == 0) red[wave] = v;
   __syncthreads();
   if (threadIdx.x != 0) return;
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) all = join<MAX>(all, red[w]);
-  *total = all;
-  write_result(all, MAX, max_norm, eps, result);
-  *tb.status = all < __builtin_inf() ? 0u : kStatusNonFinite;
+  for (int w = 1; w < kWaves; ++w) v = join<MAX>(v, red[w]);
+  *total = v;
+  write_result(v, MAX, max_norm, eps, result);
+  *tb.status = v < __builtin_inf() ? 0u : kStatusNonFinite;
 }
 
 __global__ void k_clip_coef(const double* total, int max, double max_norm, double eps, float* result) {
@@ -287,11 +251,8 @@ static void grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool 
     if (past) hipLaunchKernelGGL((k_grad_parts<MAX, true>), dim3(parts), dim3(kThreads), 0, st, tb);
     else hipLaunchKernelGGL((k_grad_parts<MAX, false>), dim3(parts), dim3(kThreads), 0, st, tb);
   }
-  const bool fused = count <= kFused && parts <= kFusedParts;
-  if (!fused)
-    hipLaunchKernelGGL(k_grad_tensors<MAX>, dim3((count + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, st,
-                       tb, count, norms);
-  hipLaunchKernelGGL(k_grad_total<MAX>, dim3(1), dim3(kWaves * 64), 0, st, tb, count, (int)fused, max_norm, eps, total,
+  const uint32_t groups = 1 + (norms ? (count + kWaves - 1) / kWaves : 0);
+  hipLaunchKernelGGL(k_grad_total<MAX>, dim3(groups), dim3(kWaves * 64), 0, st, tb, count, parts, max_norm, eps, total,
                      norms, result);
 }
 hipError_t launch_grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool past, bool max, double max_norm,

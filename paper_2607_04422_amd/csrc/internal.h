@@ -408,7 +408,7 @@ struct GradTable {
   uint32_t* status;
   GradRef* tensors;        // one more than there are: the last holds the number of parts in `first`
   GradPart* parts;
-  double *sums, *partial;
+  double* partial;         // one a part
 };
 // Tensors by value, for the launches that write the table.
 constexpr int kMaxGradChunk = 48;
