@@ -524,10 +524,10 @@ def _launch_stream(device, stream) -> int:
 
 def _call(fn, device, *args) -> int:
     """fn(*args) with `device` current: kernels are launched on the current GPU's code."""
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return fn(*args)
-    return fn(*args)
+    if device.index == torch._C._cuda_getDevice():
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
 
 
 def _as_rows(t: torch.Tensor, name: str):
@@ -691,13 +691,11 @@ class RmsNormOutput(NamedTuple):
 
 def _matrix(t: torch.Tensor, name: str, like: torch.Tensor = None):
     """(rows, row stride) of a tensor whose last dimension is contiguous and whose others are
-    rows of one stride; checked against `like` for type, shape and GPU."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a GPU tensor")
-    shape = t.shape
-    if like is not None and (t.dtype is not like.dtype or shape != like.shape or t.device != like.device):
+    rows of one stride; checked against `like`, an accepted one, for type, shape and GPU."""
+    if like is not None and (not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.shape != like.shape or
+                             t.device != like.device):
         raise TypeError(f"{name} must have x's type, shape and GPU")
-    cols = shape[-1]
+    cols = t.shape[-1]
     if t.is_contiguous():
         return (t.numel() // cols if cols else 0), cols
     if t.shape[-1] > 1 and t.stride(-1) != 1:
@@ -718,11 +716,12 @@ def _matrix(t: torch.Tensor, name: str, like: torch.Tensor = None):
 def _gain_type(gain, x):
     if gain is None:
         return FLOAT32
-    if not isinstance(gain, torch.Tensor) or gain.device != x.device or gain.dtype not in _GAIN_TYPES:
+    code = _GAIN_TYPES.get(gain.dtype) if isinstance(gain, torch.Tensor) and gain.device == x.device else None
+    if code is None:
         raise TypeError("gain must be a float32 or bfloat16 tensor on x's GPU")
-    if gain.dim() != 1 or gain.shape[0] != x.shape[-1] or not gain.is_contiguous():
+    if gain.shape != x.shape[-1:] or not gain.is_contiguous():
         raise ValueError("gain must be a contiguous vector of x's columns")
-    return _GAIN_TYPES[gain.dtype]
+    return code
 
 
 def _need_stream(x, name: str) -> int:
@@ -731,11 +730,12 @@ def _need_stream(x, name: str) -> int:
         load()
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if x.dtype not in _TYPES:
+    code = _TYPES.get(x.dtype)
+    if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16")
     if x.dim() < 1:
         raise ValueError(f"{name} must have a dimension of columns")
-    return _TYPES[x.dtype]
+    return code
 
 
 def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residual: torch.Tensor = None,
@@ -755,9 +755,9 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     ld_r = _matrix(residual, "residual", x)[1] if residual is not None else 0
     raw = _launch_stream(dev, stream)
     if out is None:
-        codes = scales = y = None
         # empty_like keeps a stride, and is the cheaper call
         packed = ld_x == cols and x.is_contiguous()
+        codes = scales = y = None
         if quantize:
             codes = torch.empty_like(x, dtype=torch.uint8) if packed else x.new_empty(shape, dtype=torch.uint8)
             scales = x.new_empty((*lead, -(-cols // group)) if group > 0 else lead,
