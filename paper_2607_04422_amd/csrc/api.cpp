@@ -1510,7 +1510,7 @@ size_t carve_grad_list(void* base, int64_t count, int64_t parts, GradTable& w) {
 }
 
 // What a list's passes read past the caches (fp4root_grad_list::flags).  A list that fits in the
-// L2 caches together leaves there what its next pass reads (12 parameters of 3.9 M elements:
+// L2 caches together leaves there what its next pass reads (12 parameters of 2.0 M elements:
 // 12.4 us clipped, 15.2 past them).  A larger one does not, and its loads run faster past them:
 // the norm of 2.8 GB 467 -> 415 us, of 227 MB 45 -> 39.  The norm of a list with outputs elsewhere
 // stays in, since its second pass then finds more in the last-level cache (354 M BF16 elements

@@ -60,7 +60,7 @@ FP4R_DEV double block_join(double v) {
 // Walks vectors [v0, v1) (of 16 bytes of the input) of a tensor.  A contiguous one goes in
 // steps of kUnroll vectors of VE elements a thread, so that as many loads are in flight:
 // load(offset) fetches one, use(raw, offset) consumes it (the norm of 2.8 GB: 478 -> 460 us,
-// twelve parameters of 3.9 M elements 9.2 -> 5.2).  The rest, and tensors of rows, go through
+// twelve parameters of 2.0 M elements 9.2 -> 5.2).  The rest, and tensors of rows, go through
 // one(first element's offset in the input, ... in the output, count).
 constexpr int kUnroll = 4;
 template <class TI, int VE, class L, class U, class F>

@@ -69,7 +69,7 @@ FP4R_DEV void unpack_raw(const V& w, float (&x)[N]) {
 }
 // N values as 16-byte vectors (4 of a 16-bit type: one of 8 bytes), past the caches: what is
 // written once and not read by the same kernel displaces nothing (clipping 354 M BF16 elements
-// into FP32 551 -> 501 us, twelve parameters of 3.9 M elements 12.6 -> 12.1).
+// into FP32 551 -> 501 us, twelve parameters of 2.0 M elements 12.6 -> 12.1).
 template <class T, int N>
 FP4R_DEV void store_full(T* p, const float (&x)[N]) {
   if constexpr (sizeof(T) == 4) {

@@ -574,11 +574,11 @@ class GradClipper:
 
     def __init__(self, grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6,
                  measure_only: bool = False):
-        self._make(grads, max_norm, outputs, norm_type, eps, measure_only, None)
+        self._make(grads, max_norm, outputs, norm_type, eps, measure_only)
         if self.count:
             torch.cuda.current_stream(self.device).synchronize()
 
-    def _make(self, grads, max_norm, outputs, norm_type, eps, measure_only, stream):
+    def _make(self, grads, max_norm, outputs, norm_type, eps, measure_only):
         lib = load()
         self.grads = list(grads)
         self.outputs = list(outputs) if outputs is not None else self.grads
@@ -614,7 +614,7 @@ class GradClipper:
         self.total_norm, self.coef = self.result[0], self.result[1]
         self.list = GradList()
         _check(_call(lib.fp4root_grad_list_init, self.device, ctypes.byref(self.list), tensors, n, _ptr(self.ws),
-                     self.ws.numel(), _launch_stream(self.device, stream)), "fp4root_grad_list_init")
+                     self.ws.numel(), _launch_stream(self.device, None)), "fp4root_grad_list_init")
         self._list = ctypes.byref(self.list)
         self._norm_args = (self._list, self.kind, self.max_norm, self.eps, _ptr(self.total),
                            _ptr(self.norms) if n else None, _ptr(self.result))
@@ -668,13 +668,12 @@ def fp4root_clip_grads(grads, max_norm: float, outputs=None, norm_type=2, eps: f
     """Clip a list of gradient tensors by their global norm, in place or into `outputs`; returns
     the norm before clipping (a float32 GPU scalar).  A program that clips the same buffers step
     after step keeps a GradClipper instead."""
+    if stream is not None:        # allocated where it is used
+        with torch.cuda.stream(stream):
+            return fp4root_clip_grads(grads, max_norm, outputs, norm_type, eps)
     c = GradClipper.__new__(GradClipper)
-    c._make(grads, max_norm, outputs, norm_type, eps, False, stream)
-    if stream is not None:                 # the memory was allocated, and cleared, on the current stream
-        for t in (c.ws, c.total, c.norms, c.result):
-            t.record_stream(stream)
-        stream.wait_stream(torch.cuda.current_stream(c.device))
-    c(stream)
+    c._make(grads, max_norm, outputs, norm_type, eps, False)
+    c()
     return c.total_norm
 
 
@@ -747,13 +746,16 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     float16, rows of one stride; out: an earlier call's result, whose tensors are written again
     (h may be the residual or x itself: in place); status: an int32 GPU tensor of one element.
     See fp4root_rmsnorm_quantize in include/fp4root.h."""
+    if stream is not None:        # allocated where it is used
+        with torch.cuda.stream(stream):
+            return fp4root_rmsnorm_quantize(x, gain, residual, eps, group, e8m0, quantize, want_y, out, status)
     type_ = _need_stream(x, "x")
     gain_type = _gain_type(gain, x)
     rows, ld_x = _matrix(x, "x")
     shape, dev = x.shape, x.device
     lead, cols = shape[:-1], shape[-1]
     ld_r = _matrix(residual, "residual", x)[1] if residual is not None else 0
-    raw = _launch_stream(dev, stream)
+    raw = _launch_stream(dev, None)
     if out is None:
         # empty_like keeps a stride, and is the cheaper call
         packed = ld_x == cols and x.is_contiguous()
@@ -769,10 +771,6 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
             y = x.new_empty(shape)
         out = RmsNormOutput(codes, scales, rstd, h, y)
         ld_h = ld_y = cols
-        if stream is not None:
-            for t in out:
-                if t is not None and t is not x:
-                    t.record_stream(stream)
     else:
         codes, scales, rstd, h, y = out
         for name, t, dtype, want in (("codes", codes, torch.uint8, shape),
@@ -804,6 +802,9 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     """(dx, dgain) of the norm of h under the gradient dy of its output and dh of h itself; dx in
     h's type is the gradient of x and of the residual alike, dgain is float32.  dx may be given
     (dy, h or dh itself: in place); see fp4root_rmsnorm_backward in include/fp4root.h."""
+    if stream is not None:        # allocated where it is used
+        with torch.cuda.stream(stream):
+            return fp4root_rmsnorm_backward(dy, h, gain, rstd, dh, dx, dgain, want_dgain, ws)
     type_ = _need_stream(h, "h")
     rows, ld_h = _matrix(h, "h")
     ld_dy = _matrix(dy, "dy", h)[1]
@@ -813,18 +814,15 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     _need_gpu_f32(rstd, "rstd")
     if rstd.numel() != rows or not rstd.is_contiguous() or rstd.device != dev:
         raise ValueError("rstd must hold one contiguous element per row on h's GPU")
-    raw = _launch_stream(dev, stream)
-    new = []
+    raw = _launch_stream(dev, None)
     if dx is None:
         dx = torch.empty_like(h) if ld_h == cols and h.is_contiguous() else h.new_empty(h.shape)
         ld_dx = cols
-        new.append(dx)
     else:
         ld_dx = _matrix(dx, "dx", h)[1]
     need = 0
     if dgain is None and want_dgain:
         dgain = h.new_empty(cols, dtype=torch.float32)
-        new.append(dgain)
     if dgain is not None:
         _need_gpu_f32(dgain, "dgain")
         if dgain.numel() != cols or not dgain.is_contiguous() or dgain.device != dev:
@@ -832,12 +830,8 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
         need = _lib.fp4root_rmsnorm_backward_workspace(rows, cols)
         if ws is None:
             ws = h.new_empty(need, dtype=torch.uint8)
-            new.append(ws)
         elif ws.device != dev or not ws.is_contiguous():
             raise ValueError("ws must be contiguous on h's GPU")
-    if stream is not None:
-        for t in new:
-            t.record_stream(stream)
     _check(_call(_lib.fp4root_rmsnorm_backward, dev, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h,
                  dh.data_ptr() if dh is not None else None, ld_dh, gain.data_ptr() if gain is not None else None,
                  rstd.data_ptr(), dx.data_ptr(), ld_dx, dgain.data_ptr() if dgain is not None else None, rows, cols,

@@ -291,7 +291,13 @@ def test_graph_replay_and_streams():
 def test_function_in_place():
     grads = make([(100, 7), (3,)], torch.float32, 13)
     want = [g.clone() for g in grads]
+    other = [g.clone() for g in grads]
     norm = F.fp4root_clip_grads(grads, 0.25)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    again = F.fp4root_clip_grads(other, 0.25, stream=side)
+    torch.cuda.synchronize()
+    assert float(again) == float(norm) and all(torch.equal(a, b) for a, b in zip(other, grads))
     ref = torch.cat([w.reshape(-1) for w in want]).double().norm()
     assert float(norm) == pytest.approx(float(ref), rel=1e-6)
     coef = torch.tensor(min(1.0, 0.25 / (float(ref) + 1e-6)), dtype=torch.float32)

@@ -157,11 +157,18 @@ def test_non_finite_rows_stay_alone():
     # an infinite gain: its group's codes are not numbers, the others' are
     gain = torch.ones(200, device="cuda")
     gain[40] = math.inf
-    status.zero_()
-    o = F.fp4root_rmsnorm_quantize(x, gain, group=32, status=status)
-    assert int(status) == -4
-    assert bool(((o.codes[:, 40] & 0x7F) == 0x7F).all())
-    assert torch.equal(o.codes[:, 64:], F.fp4root_rmsnorm_quantize(x, None, group=32).codes[:, 64:])
+    for e8m0 in (False, True):
+        status.zero_()
+        o = F.fp4root_rmsnorm_quantize(x, gain, group=32, e8m0=e8m0, status=status)
+        assert int(status) == -4
+        assert bool(((o.codes[:, 40] & 0x7F) == 0x7F).all())
+        plain = F.fp4root_rmsnorm_quantize(x, None, group=32, e8m0=e8m0)
+        assert torch.equal(o.codes[:, 64:], plain.codes[:, 64:])
+        # a gain that is no number: its own codes are none either
+        nan = torch.where(torch.isinf(gain), math.nan, gain)
+        o = F.fp4root_rmsnorm_quantize(x, nan, group=32, e8m0=e8m0)
+        assert bool(((o.codes[:, 40] & 0x7F) == 0x7F).all())
+        assert torch.equal(o.codes[:, 64:], plain.codes[:, 64:])
 
 
 @pytest.mark.parametrize("dtype", TYPES)
