@@ -79,13 +79,39 @@ FP4R_DEV void each_vector(const GradRef& t, int64_t v0, int64_t v1, L load, U us
     for (; i < end; i += kThreads * VE) one(i, i, (int)min((int64_t)VE, end - i));
     return;
   }
-  const int64_t per_row = (t.cols + VI - 1) / VI;
-  for (int64_t v = v0 + threadIdx.x; v < v1; v += kThreads) {
-    const int64_t row = v / per_row, c = (v - row * per_row) * VI;
-    const int n = (int)min((int64_t)VI, t.cols - c);
+  // rows: the same with each vector's place found by division, in 32 bits where they are enough
+  constexpr int R = VI / VE;
+  const uint32_t per_row = (uint32_t)((t.cols + VI - 1) / VI);   // cols < 2^33, see kMaxLd
+  const bool narrow = t.vectors >> 32 == 0;
+  int64_t v = v0 + threadIdx.x;
+  while (v < v1) {
+    int64_t i[kUnroll], o[kUnroll];
+    int n[kUnroll];
+    bool full = true;
 #pragma unroll
-    for (int k = 0; k < VI; k += VE)
-      if (k < n) one(row * t.ld_in + c + k, row * t.ld_out + c + k, min(VE, n - k));
+    for (int u = 0; u < kUnroll; ++u) {
+      const int64_t w = v + u * kThreads;
+      const int64_t row = narrow ? (int64_t)((uint32_t)w / per_row) : w / per_row;
+      const int64_t c = (w - row * per_row) * VI;
+      i[u] = row * t.ld_in + c;
+      o[u] = row * t.ld_out + c;
+      n[u] = w < v1 ? (int)min((int64_t)VI, t.cols - c) : 0;
+      full = full && n[u] == VI;
+    }
+    if (full) {
+      decltype(load(0)) raw[kUnroll * R];
+#pragma unroll
+      for (int u = 0; u < kUnroll * R; ++u) raw[u] = load(i[u / R] + (u % R) * VE);
+#pragma unroll
+      for (int u = 0; u < kUnroll * R; ++u) use(raw[u], o[u / R] + (u % R) * VE);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUnroll * R; ++u) {
+        const int k = (u % R) * VE, m = n[u / R] - k;
+        if (m > 0) one(i[u / R] + k, o[u / R] + k, min(VE, m));
+      }
+    }
+    v += kUnroll * kThreads;
   }
 }
 

@@ -438,6 +438,7 @@ struct RmsArgs {
   int32_t cols, group, groups;   // group: columns a scale covers, 0 for the row; groups: scales a row
   int32_t type, gain_f32, e8m0;
   int32_t x_past;          // x is read past the caches
+  int32_t tpr;             // threads a row (the launch's choice)
   double eps;
 };
 hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st);
@@ -450,6 +451,7 @@ struct RmsBwdArgs {
   float* partial;          // rms_bwd_groups(rows, cols) rows of cols
   int64_t rows, ld_dy, ld_h, ld_dh, ld_dx;
   int32_t cols, type, gain_f32;
+  int32_t tpr;             // threads a row (the launch's choice)
 };
 // Workgroups of the first pass, each with one partial row of the gain's gradient.
 int64_t rms_bwd_groups(int64_t rows, int64_t cols);

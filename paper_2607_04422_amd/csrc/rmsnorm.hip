@@ -8,8 +8,11 @@
 //   g = dy gain,  xhat = h rstd,  c = mean(g xhat),  dx = rstd (g - xhat c) + dh,
 //   dgain = sum over rows of dy xhat
 // Both passes are bound by memory: a row is read once and stays in registers.  A thread holds
-// vectors of 8 columns, TPR of them apart, so a group of columns lies in 4, 8 or 16 adjacent
-// lanes.  TPR threads share a row.
+// VPT vectors of 8 columns, as many vectors apart as threads share the row, so a group of columns
+// lies in 4, 8 or 16 adjacent lanes.  A row takes whole waves, or 16 or 32 lanes of one where it
+// is narrow (the heads of an attention: 32768 x 96 BF16 19.4 -> 10.2 us, its gradients 25.2 ->
+// 17.9); with a row in whole waves their number fits the row, not the next power of two (8192 x 4099
+// 81.6 -> 75 and 111.4 -> 93).
 #include "device.h"
 #include "internal.h"
 #include "vec.h"
@@ -39,12 +42,31 @@ FP4R_DEV float wave_max(float v) {
   v = group_max(v, 16);
   return fmaxf(fmaxf(lane_f(v, 0), lane_f(v, 16)), fmaxf(lane_f(v, 32), lane_f(v, 48)));
 }
-FP4R_DEV float wave_sum(float v) {
+// Sums over the lanes of a row: SUB lanes (16 or 32), or the wave for SUB 0.
+template <int SUB>
+FP4R_DEV float lanes_sum(float v) {
   v = v + dpp_f<0xB1>(v);
   v = v + dpp_f<0x4E>(v);
   v = v + dpp_f<0x141>(v);
   v = v + dpp_f<0x140>(v);
-  return (lane_f(v, 0) + lane_f(v, 16)) + (lane_f(v, 32) + lane_f(v, 48));
+  if constexpr (SUB == 16) return v;
+  else if constexpr (SUB == 32) return v + __shfl_xor(v, 16);
+  else return (lane_f(v, 0) + lane_f(v, 16)) + (lane_f(v, 32) + lane_f(v, 48));
+}
+template <int SUB>
+FP4R_DEV double lanes_sum(double v) {
+  if constexpr (SUB == 0) return wave_sum_d(v);
+  v = v + dpp_d<0xB1>(v);
+  v = v + dpp_d<0x4E>(v);
+  v = v + dpp_d<0x141>(v);
+  v = v + dpp_d<0x140>(v);
+  return SUB == 16 ? v : v + __shfl_xor(v, 16);
+}
+template <int SUB>
+FP4R_DEV float lanes_max(float v) {
+  if constexpr (SUB == 0) return wave_max(v);
+  v = group_max(v, 16);
+  return SUB == 16 ? v : fmaxf(v, __shfl_xor(v, 16));
 }
 
 // 1 / sqrt(a) for 0 < a < 2^1000: the instruction's estimate and two Newton steps.
@@ -115,15 +137,17 @@ FP4R_DEV void store_codes(uint8_t* p, int n, const float (&y)[8], float inv) {
   }
 }
 
-template <class T, int TPR, int VPT>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
-  constexpr int WPR = TPR / 64;                       // waves a row
-  constexpr int RPG = TPR < 256 ? 256 / TPR : 1;      // rows a workgroup
-  __shared__ double red_s[RPG][WPR];
-  __shared__ float red_m[RPG][WPR];
-  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * RPG + slot;
-  const bool live = RPG == 1 || row < a.rows;
+// SUB: lanes a row, or 0 for whole waves (a.tpr threads; a workgroup holds as many rows as fit).
+template <class T, int VPT, int SUB>
+__global__ __launch_bounds__(1024) void k_rmsnorm(RmsArgs a) {
+  __shared__ double red_s[16];                        // one a wave
+  __shared__ float red_m[16];
+  const int TPR = SUB ? SUB : a.tpr;
+  const int slot = threadIdx.x / TPR, t = threadIdx.x - slot * TPR, slots = blockDim.x / TPR;
+  const int wpr = TPR / 64, wave0 = slot * wpr;       // waves a row (0: less than one), the row's first
+  const int lane16 = threadIdx.x & 15;                // takes a wave's part: every 16 lanes join them all
+  const int64_t row = (int64_t)blockIdx.x * slots + slot;
+  const bool live = row < a.rows;
   const int cols = live ? a.cols : 0;                 // a slot past the last row reads and writes nothing
   Raw8<T> h[VPT];
 #pragma unroll
@@ -168,13 +192,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) s = __builtin_fma((double)u[k], (double)u[k], s);
   }
-  s = wave_sum_d(s);
-  if constexpr (WPR > 1) {
-    if ((t & 63) == 0) red_s[slot][t >> 6] = s;
+  s = lanes_sum<SUB>(s);
+  if (wpr > 1) {
+    if ((threadIdx.x & 63) == 0) red_s[threadIdx.x >> 6] = s;
     __syncthreads();
-    s = red_s[slot][0];
-#pragma unroll
-    for (int w = 1; w < WPR; ++w) s += red_s[slot][w];
+    s = lanes_sum<16>(lane16 < wpr ? red_s[wave0 + lane16] : 0.0);
   }
   const float rstd = (float)rsqrt64(s / (double)a.cols + a.eps);
   if (t == 0 && live) {
@@ -217,13 +239,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
     top = fmaxf(top, m);
   }
   if (!a.codes || lanes) return;
-  top = wave_max(top);
-  if constexpr (WPR > 1) {
-    if ((t & 63) == 0) red_m[slot][t >> 6] = top;
+  top = lanes_max<SUB>(top);
+  if (wpr > 1) {
+    if ((threadIdx.x & 63) == 0) red_m[threadIdx.x >> 6] = top;
     __syncthreads();
-    top = red_m[slot][0];
-#pragma unroll
-    for (int w = 1; w < WPR; ++w) top = fmaxf(top, red_m[slot][w]);
+    top = lanes_max<16>(lane16 < wpr ? red_m[wave0 + lane16] : 0.0f);
   }
   uint32_t stored;
   const float inv = scale_of(top, a.e8m0, stored);
@@ -241,11 +261,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm(RmsArgs a) {
   }
 }
 
-template <class T, int TPR, int VPT>
-void run_rmsnorm(const RmsArgs& a, hipStream_t st) {
-  constexpr int NT = TPR < 256 ? 256 : TPR, RPG = NT / TPR;
-  hipLaunchKernelGGL((k_rmsnorm<T, TPR, VPT>), dim3((uint32_t)((a.rows + RPG - 1) / RPG)), dim3(NT), 0, st, a);
+template <class T, int VPT, int SUB>
+void run_rmsnorm(RmsArgs a, int tpr, int slots, hipStream_t st) {
+  a.tpr = tpr;
+  hipLaunchKernelGGL((k_rmsnorm<T, VPT, SUB>), dim3((uint32_t)((a.rows + slots - 1) / slots)), dim3(tpr * slots), 0, st,
+                     a);
 }
+
+// Whole waves that hold v vectors.
+int wave_threads(int64_t v) { return (int)((v + 63) / 64 * 64); }
 
 // Many rows: 8 or 16 columns a thread (8192 x 4096: 2 vectors of 256 threads 42.3 us, 1 of 512
 // 44.0, 4 of 128 44.4, 8 of 64 49.5; 16384 x 8192: 2 of 512 160, 4 of 256 161, 1 of 1024 188).
@@ -255,16 +279,16 @@ void run_rmsnorm(const RmsArgs& a, hipStream_t st) {
 constexpr int64_t kFewRows = 512;
 template <class T>
 void pick_rmsnorm(const RmsArgs& a, hipStream_t st) {
+  const int64_t v = (a.cols + 7) / 8;
   const bool few = a.rows <= kFewRows;
-  if (a.cols <= 512) run_rmsnorm<T, 64, 1>(a, st);
-  else if (a.cols <= 1024) run_rmsnorm<T, 128, 1>(a, st);
-  else if (a.cols <= 2048) run_rmsnorm<T, 256, 1>(a, st);
-  else if (a.cols <= 4096 && few) run_rmsnorm<T, 512, 1>(a, st);
-  else if (a.cols <= 4096) run_rmsnorm<T, 256, 2>(a, st);
-  else if (a.cols <= 8192 && few) run_rmsnorm<T, 1024, 1>(a, st);
-  else if (a.cols <= 8192) run_rmsnorm<T, 512, 2>(a, st);
-  else if (a.cols <= 16384) run_rmsnorm<T, 1024, 2>(a, st);
-  else run_rmsnorm<T, 1024, 4>(a, st);
+  if (v <= 16) return run_rmsnorm<T, 1, 16>(a, 16, 16, st);
+  if (v <= 32) return run_rmsnorm<T, 1, 32>(a, 32, 8, st);
+  if (v <= 256 || (v <= 1024 && few)) {
+    const int tpr = wave_threads(v);
+    return run_rmsnorm<T, 1, 0>(a, tpr, tpr <= 128 ? 256 / tpr : 1, st);
+  }
+  if (v <= 2048) return run_rmsnorm<T, 2, 0>(a, wave_threads((v + 1) / 2), 1, st);
+  run_rmsnorm<T, 4, 0>(a, wave_threads((v + 3) / 4), 1, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -272,19 +296,18 @@ void pick_rmsnorm(const RmsArgs& a, hipStream_t st) {
 // its columns' part of dgain in registers; at the end the slots are added in LDS and the
 // workgroup writes one row of partials, which k_rms_dgain adds in order.
 
-// Threads of a workgroup: 512, or a row's where it takes more (1024 threads for all widths:
-// 8192 x 2048 31.0 us for 29.0, 8192 x 4096 58.0 for 56.0).
-constexpr int bwd_threads(int tpr) { return tpr < 512 ? 512 : tpr; }
-
-template <class T, int TPR, int VPT>
-__global__ __launch_bounds__(bwd_threads(TPR)) void k_rms_bwd(RmsBwdArgs a) {
-  constexpr int NT = bwd_threads(TPR), RPG = NT / TPR, WPR = TPR / 64;
-  __shared__ float red[2][NT / 64];
-  __shared__ float slab[RPG > 1 ? NT * 8 : 1];
-  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
-  float acc[VPT][8];
+// SUB as above; MAXT: the most threads of a workgroup; GAIN: with dgain (the widest rows leave it
+// to k_rms_cols, since the registers do not hold them beside their part of it, and read dh late).
+template <class T, int VPT, int SUB, int MAXT, bool GAIN>
+__global__ __launch_bounds__(MAXT) void k_rms_bwd(RmsBwdArgs a) {
+  __shared__ float red[2][MAXT / 64];
+  __shared__ float slab[VPT == 1 ? 512 * 8 : 1];      // only rows of up to 256 threads share a workgroup
+  const int TPR = SUB ? SUB : a.tpr;
+  const int slot = threadIdx.x / TPR, t = threadIdx.x - slot * TPR, RPG = blockDim.x / TPR;
+  const int wpr = TPR / 64, wave0 = slot * wpr, lane16 = threadIdx.x & 15;
+  float acc[GAIN ? VPT : 1][8];
 #pragma unroll
-  for (int i = 0; i < VPT; ++i)
+  for (int i = 0; i < (GAIN ? VPT : 1); ++i)
 #pragma unroll
     for (int k = 0; k < 8; ++k) acc[i][k] = 0.0f;
   const float inv_cols = 1.0f / (float)a.cols;
@@ -296,14 +319,14 @@ __global__ __launch_bounds__(bwd_threads(TPR)) void k_rms_bwd(RmsBwdArgs a) {
     // read soon: h passes the caches, and so does dx, which is written after all that is read
     // (8192 x 4096 BF16: 57.0 us with nothing past them, 55.0 so, and 16384 x 8192: 197, 194;
     // with dy and dh past them too, 2048 x 4096, which fit: 22.6 us for 19.6)
-    Raw8<T> h[VPT], d[VPT], e[VPT];
+    Raw8<T> h[VPT], d[VPT], e[GAIN ? VPT : 1];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int c = (i * TPR + t) * 8, n = live ? min(8, a.cols - c) : 0;
       h[i] = load_raw8<T, true>((const T*)a.h + row * a.ld_h + c, n);
       d[i] = load_raw8((const T*)a.dy + row * a.ld_dy + c, n);
     }
-    if (a.dh) {
+    if (GAIN && a.dh) {
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         const int c = (i * TPR + t) * 8, n = live ? min(8, a.cols - c) : 0;
@@ -327,17 +350,15 @@ __global__ __launch_bounds__(bwd_threads(TPR)) void k_rms_bwd(RmsBwdArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float xhat = x[k] * rstd;
-        acc[i][k] = fmaf(y[k], xhat, acc[i][k]);
+        if (GAIN) acc[GAIN ? i : 0][k] = fmaf(y[k], xhat, acc[GAIN ? i : 0][k]);
         dot = fmaf(y[k] * g[k], xhat, dot);
       }
     }
-    dot = wave_sum(dot);
-    if constexpr (WPR > 1) {
+    dot = lanes_sum<SUB>(dot);
+    if (wpr > 1) {
       if ((threadIdx.x & 63) == 0) red[side][threadIdx.x >> 6] = dot;
       __syncthreads();   // two sides: the next row's values do not overtake this row's readers
-      dot = red[side][slot * WPR];
-#pragma unroll
-      for (int w = 1; w < WPR; ++w) dot += red[side][slot * WPR + w];
+      dot = lanes_sum<16>(lane16 < wpr ? red[side][wave0 + lane16] : 0.0f);
     }
     const float mean = dot * inv_cols;
 #pragma unroll
@@ -356,31 +377,70 @@ __global__ __launch_bounds__(bwd_threads(TPR)) void k_rms_bwd(RmsBwdArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) o[k] = rstd * (y[k] * g[k] - (x[k] * rstd) * mean);
       if (a.dh) {
-        unpack8(e[i], x);
+        if constexpr (!GAIN) e[0] = load_raw8((const T*)a.dh + row * a.ld_dh + c, n);
+        unpack8(e[GAIN ? i : 0], x);
 #pragma unroll
         for (int k = 0; k < 8; ++k) o[k] += x[k];
       }
       store_raw8<T, true>((T*)a.dx + row * a.ld_dx + c, n, pack8<T>(o));
     }
   }
-  if (!a.dgain) return;
+  if (!GAIN || !a.dgain) return;
   float* out = a.partial + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int c = (i * TPR + t) * 8, n = min(8, a.cols - c);
-    if constexpr (RPG > 1) {
+    if (VPT == 1 && RPG > 1) {
       __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 8; ++k) slab[(slot * 8 + k) * TPR + t] = acc[i][k];
+      for (int k = 0; k < 8; ++k) slab[(slot * 8 + k) * TPR + t] = acc[GAIN ? i : 0][k];
       __syncthreads();
       if (slot == 0) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          for (int q = 1; q < RPG; ++q) acc[i][k] += slab[(q * 8 + k) * TPR + t];
+          for (int q = 1; q < RPG; ++q) acc[GAIN ? i : 0][k] += slab[(q * 8 + k) * TPR + t];
       }
     }
-    if (slot == 0 && n > 0) store_raw8(out + c, n, pack8<float>(acc[i]));
+    if (slot == 0 && n > 0) store_raw8(out + c, n, pack8<float>(acc[GAIN ? i : 0]));
   }
+}
+
+// dgain of the widest rows: 512 columns of a chunk of rows a workgroup, a wave every fourth row,
+// four rows in flight.
+template <class T>
+__global__ __launch_bounds__(256) void k_rms_cols(RmsBwdArgs a, int64_t chunk) {
+  __shared__ float red[3][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 512 + lane * 8, n = min(8, a.cols - c);
+  const int64_t r1 = min(a.rows, (int64_t)(blockIdx.y + 1) * chunk);
+  float acc[8] = {};
+  for (int64_t r = (int64_t)blockIdx.y * chunk + wave; r < r1; r += 16) {
+    Raw8<T> h[4], d[4];
+    float rstd[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t row = r + 4 * u;
+      const int m = row < r1 ? n : 0;
+      h[u] = load_raw8((const T*)a.h + row * a.ld_h + c, m);
+      d[u] = load_raw8((const T*)a.dy + row * a.ld_dy + c, m);
+      rstd[u] = row < r1 ? a.rstd[row] : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float x[8], y[8];
+      unpack8(h[u], x);
+      unpack8(d[u], y);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc[k] = fmaf(y[k], x[k] * rstd[u], acc[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (wave) red[wave - 1][k * 64 + lane] = acc[k];
+  __syncthreads();
+  if (wave || n <= 0) return;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) acc[k] += (red[0][k * 64 + lane] + red[1][k * 64 + lane]) + red[2][k * 64 + lane];
+  store_raw8(a.partial + (int64_t)blockIdx.y * a.cols + c, n, pack8<float>(acc));
 }
 
 // 16 columns by 64 slices of the partial rows a workgroup: each thread adds four columns of
@@ -411,35 +471,51 @@ __global__ __launch_bounds__(256) void k_rms_dgain(const float* partial, int cou
   if (l == 0 && blockIdx.x * 16 + col < cols) dgain[blockIdx.x * 16 + col] = v;
 }
 
-// Threads and vectors a row.  A thread keeps 8 columns where 512 threads cover the row, so that
-// 4 to 6 waves fit a SIMD (16384 x 8192: 2 vectors of 512 threads 197 us, 4 of 256 222, 1 of
-// 1024 209; 8192 x 4096: 1 of 512 56.0, 2 of 256 56.8, 4 of 128 66.8).
+// Threads a row, vectors a thread and rows a workgroup.  A thread keeps 8 columns where 768
+// threads cover the row, so that 4 to 6 waves fit a SIMD (8192 x 4096: 1 vector of 512 threads
+// 56.0 us, 2 of 256 56.8, 4 of 128 66.8; 8192 x 5120 1 of 640 69.1, 2 of 320 72.3; 8192 x 7168
+// the same; 16384 x 8192 2 of 512 197, 4 of 256 222, 1 of 1024 209), and narrow rows share
+// workgroups of 512 threads (1024: 8192 x 2048 31.0 us for 29.0).  Rows past 16384 columns
+// leave dgain to a pass of its own (with it the registers spill: 4096 x 20000 250 us, so 217).
 struct BwdShape {
-  int tpr, vpt;
+  int tpr, vpt, slots;
 };
 BwdShape bwd_shape(int64_t cols) {
-  const int tpr = cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 8192 ? 512 : 1024;
-  const int64_t v = (cols + 8 * tpr - 1) / (8 * tpr);
-  return {tpr, v <= 1 ? 1 : v <= 2 ? 2 : 4};
+  const int64_t v = (cols + 7) / 8;
+  if (v <= 16) return {16, 1, 32};
+  if (v <= 32) return {32, 1, 16};
+  if (v <= 768) {
+    const int tpr = wave_threads(v);
+    return {tpr, 1, tpr <= 512 ? 512 / tpr : 1};
+  }
+  if (v <= 2048) return {wave_threads((v + 1) / 2), 2, 1};
+  return {wave_threads((v + 3) / 4), 4, 1};
+}
+
+// k_rms_cols: its chunks of rows, about 2048 workgroups of at least 64 rows.
+int64_t col_chunk(int64_t rows, int64_t cols) {
+  const int64_t chunks = 2048 / ((cols + 511) / 512), chunk = (rows + chunks - 1) / chunks;
+  return chunk < 64 ? 64 : chunk;
 }
 
 template <class T>
-void run_bwd(const RmsBwdArgs& a, uint32_t grid, hipStream_t st) {
+void run_bwd(RmsBwdArgs a, uint32_t grid, hipStream_t st) {
   const BwdShape s = bwd_shape(a.cols);
-  const dim3 nt(bwd_threads(s.tpr));
-#define FP4R_BWD(TPR, VPT)                                                              \
-  if (s.tpr == TPR && s.vpt == VPT) {                                                   \
-    hipLaunchKernelGGL((k_rms_bwd<T, TPR, VPT>), dim3(grid), nt, 0, st, a);             \
-    return;                                                                             \
+  const dim3 nt(s.tpr * s.slots);
+  a.tpr = s.tpr;
+  if (s.tpr == 16) hipLaunchKernelGGL((k_rms_bwd<T, 1, 16, 512, true>), dim3(grid), nt, 0, st, a);
+  else if (s.tpr == 32) hipLaunchKernelGGL((k_rms_bwd<T, 1, 32, 512, true>), dim3(grid), nt, 0, st, a);
+  else if (s.vpt == 1) hipLaunchKernelGGL((k_rms_bwd<T, 1, 0, 768, true>), dim3(grid), nt, 0, st, a);
+  else if (s.vpt == 2) hipLaunchKernelGGL((k_rms_bwd<T, 2, 0, 1024, true>), dim3(grid), nt, 0, st, a);
+  else {
+    // dgain first: dx may be written over h or dy
+    if (a.dgain)
+      hipLaunchKernelGGL(k_rms_cols<T>, dim3((uint32_t)((a.cols + 511) / 512), grid), dim3(256), 0, st, a,
+                         col_chunk(a.rows, a.cols));
+    const dim3 rows(a.rows < 512 ? (uint32_t)a.rows : 512);
+    if (s.tpr <= 768) hipLaunchKernelGGL((k_rms_bwd<T, 4, 0, 768, false>), rows, nt, 0, st, a);
+    else hipLaunchKernelGGL((k_rms_bwd<T, 4, 0, 1024, false>), rows, nt, 0, st, a);
   }
-  FP4R_BWD(64, 1)
-  FP4R_BWD(128, 1)
-  FP4R_BWD(256, 1)
-  FP4R_BWD(512, 1)
-  FP4R_BWD(512, 2)
-  FP4R_BWD(1024, 2)
-  FP4R_BWD(1024, 4)
-#undef FP4R_BWD
 }
 
 }  // namespace
@@ -453,13 +529,18 @@ hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// One workgroup a CU, or two of 512 threads where each then has four turns at least: every one
-// adds a row of partials (256 and 512 workgroups: 1024 x 4096 14.9 and 17.1 us, 2048 x 4096 20.1
-// and 19.9, 4096 x 4096 32.8 and 30.4, 32768 x 128 38.5 and 25.5; 2048 x 16384, of 1024 threads,
-// 63.7 and 72.0).
+// One workgroup a CU; two, or as many as make 1024 threads, of up to 768 threads where there are
+// eight turns a CU at least: every workgroup adds a row of partials (256 and 512 workgroups:
+// 1024 x 4096 14.9 and 17.1 us, 2048 x 4096 20.1 and 19.9, 4096 x 4096 32.8 and 30.4, 32768 x 128
+// 38.5 and 25.5; 512 and 768 of 320 threads: 8192 x 2560 40.4 and 36.5; 2048 x 16384, of 1024
+// threads, 256 and 512: 63.7 and 72.0).
 int64_t rms_bwd_groups(int64_t rows, int64_t cols) {
-  const int tpr = bwd_shape(cols).tpr, slots = bwd_threads(tpr) / tpr;
-  const int64_t all = (rows + slots - 1) / slots, most = bwd_threads(tpr) == 512 && all >= 2048 ? 512 : 256;
+  const BwdShape s = bwd_shape(cols);
+  const int threads = s.tpr * s.slots;
+  if (s.vpt == 4) return (rows + col_chunk(rows, cols) - 1) / col_chunk(rows, cols);
+  const int64_t all = (rows + s.slots - 1) / s.slots;
+  int64_t most = 256;
+  if (threads <= 768 && s.vpt <= 2 && all >= 2048) most *= threads <= 341 ? 3 : 2;
   return all < most ? all : most;
 }
 

@@ -87,7 +87,8 @@ def check_forward(x, res, gain, o, group, e8m0, eps):
 
 SHAPES = [(1, 1), (1, 4096), (3, 7), (5, 8), (2, 31), (4, 33), (7, 512), (3, 513), (2, 1024), (5, 1025), (9, 2048),
           (1, 2049), (3, 4096), (2, 5003), (2, 8192), (3, 8200), (1, 16384), (2, 16391), (1, 32768), (513, 96),
-          (130, 1000)]
+          (130, 1000), (33, 129), (35, 256), (17, 257), (6, 1536), (3, 2560), (2, 6145), (520, 8193), (700, 2057),
+          (150, 16400)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -309,7 +310,7 @@ def test_backward_against_differences():
         assert abs(num - float(dgain[j])) <= 2e-5 * (1 + abs(num))
 
 
-@pytest.mark.parametrize("cols", [64, 515, 4096])
+@pytest.mark.parametrize("cols", [64, 200, 515, 4096, 8200, 16401])
 def test_backward_strides_and_in_place(cols):
     buf = randn((9, 3 * cols + 5), torch.bfloat16, 35)
     h, dy, dh = buf[:, 1:1 + cols], buf[:, cols + 2:2 * cols + 2], buf[:, 2 * cols + 3:3 * cols + 3]
