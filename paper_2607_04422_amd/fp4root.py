@@ -569,7 +569,8 @@ class GradClipper:
     (it counts twice).  RootStep, fp4root_qadamw_update and fp4root_momentum_update take `coef` as
     grad_scale and then need no scaled gradients.  Each may be captured into a HIP graph, and
     used on any stream once the object is made (it waits for its own set-up); calls of one
-    GradClipper on two streams at once race.  The gradients' memory must stay where it is.
+    GradClipper on two streams at once race.  The gradients' memory must stay where it is, and the
+    object alive, until its calls have run.
     """
 
     def __init__(self, grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6,

@@ -305,6 +305,25 @@ def test_function_in_place():
         assert torch.allclose(g, w * coef.cuda(), rtol=2 ** -22, atol=0)
 
 
+def test_function_captured():
+    """The one-call form allocates and builds its list inside the capture."""
+    grads = make([(100, 7), (70000,)], torch.bfloat16, 33)
+    outs = [torch.zeros_like(g, dtype=torch.float32) for g in grads]
+    F.fp4root_clip_grads(grads, 0.25, outputs=outs)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        norm = F.fp4root_clip_grads(grads, 0.25, outputs=outs)
+    for k in range(3):
+        grads[1].mul_(1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = float(norm), [o.clone() for o in outs]
+        assert float(F.fp4root_clip_grads(grads, 0.25, outputs=outs)) == got[0]
+        assert all(torch.equal(a, b) for a, b in zip(outs, got[1]))
+
+
 # ---- the steps that read gradients times the coefficient ----
 
 FLAGS = [6, 22, 0]
