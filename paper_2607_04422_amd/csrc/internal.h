@@ -428,6 +428,13 @@ hipError_t launch_grad_scale(const GradTable& tb, uint32_t parts, bool past, con
 // ---------------------------------------------------------------------------
 // Root-mean-square norm (rmsnorm.hip).
 constexpr int64_t kMaxNormCols = 32768;   // a row stays in the registers of one workgroup
+// How the threads of a workgroup share rows (the launch's choice): tpr threads a row, slots rows,
+// and 2^20 / tpr rounded up, which divides a thread's number by tpr (numbers below 1024: its error
+// stays below 2^-10).
+struct RowShare {
+  int32_t tpr, slots;
+  uint32_t inverse;
+};
 struct RmsArgs {
   const void *x, *r, *gain;
   void *h, *y, *scales;
@@ -438,7 +445,7 @@ struct RmsArgs {
   int32_t cols, group, groups;   // group: columns a scale covers, 0 for the row; groups: scales a row
   int32_t type, gain_f32, e8m0;
   int32_t x_past;          // x is read past the caches
-  int32_t tpr;             // threads a row (the launch's choice)
+  RowShare share;
   double eps;
 };
 hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t st);
@@ -451,7 +458,7 @@ struct RmsBwdArgs {
   float* partial;          // rms_bwd_groups(rows, cols) rows of cols
   int64_t rows, ld_dy, ld_h, ld_dh, ld_dx;
   int32_t cols, type, gain_f32;
-  int32_t tpr;             // threads a row (the launch's choice)
+  RowShare share;
 };
 // Workgroups of the first pass, each with one partial row of the gain's gradient.
 int64_t rms_bwd_groups(int64_t rows, int64_t cols);

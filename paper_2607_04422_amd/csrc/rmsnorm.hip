@@ -137,13 +137,20 @@ FP4R_DEV void store_codes(uint8_t* p, int n, const float (&y)[8], float inv) {
   }
 }
 
-// SUB: lanes a row, or 0 for whole waves (a.tpr threads; a workgroup holds as many rows as fit).
+// The row of a thread among its workgroup's.
+template <int SUB>
+FP4R_DEV int row_slot(const RowShare& s) {
+  return SUB ? threadIdx.x / (SUB ? SUB : 1) : (int)(threadIdx.x * s.inverse >> 20);
+}
+RowShare row_share(int tpr, int slots) { return RowShare{tpr, slots, ((1u << 20) + tpr - 1) / tpr}; }
+
+// SUB: lanes a row, or 0 for whole waves.
 template <class T, int VPT, int SUB>
 __global__ __launch_bounds__(1024) void k_rmsnorm(RmsArgs a) {
   __shared__ double red_s[16];                        // one a wave
   __shared__ float red_m[16];
-  const int TPR = SUB ? SUB : a.tpr;
-  const int slot = threadIdx.x / TPR, t = threadIdx.x - slot * TPR, slots = blockDim.x / TPR;
+  const int TPR = SUB ? SUB : a.share.tpr, slots = a.share.slots;
+  const int slot = row_slot<SUB>(a.share), t = threadIdx.x - slot * TPR;
   const int wpr = TPR / 64, wave0 = slot * wpr;       // waves a row (0: less than one), the row's first
   const int lane16 = threadIdx.x & 15;                // takes a wave's part: every 16 lanes join them all
   const int64_t row = (int64_t)blockIdx.x * slots + slot;
@@ -263,7 +270,7 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(RmsArgs a) {
 
 template <class T, int VPT, int SUB>
 void run_rmsnorm(RmsArgs a, int tpr, int slots, hipStream_t st) {
-  a.tpr = tpr;
+  a.share = row_share(tpr, slots);
   hipLaunchKernelGGL((k_rmsnorm<T, VPT, SUB>), dim3((uint32_t)((a.rows + slots - 1) / slots)), dim3(tpr * slots), 0, st,
                      a);
 }
@@ -302,8 +309,8 @@ template <class T, int VPT, int SUB, int MAXT, bool GAIN>
 __global__ __launch_bounds__(MAXT) void k_rms_bwd(RmsBwdArgs a) {
   __shared__ float red[2][MAXT / 64];
   __shared__ float slab[VPT == 1 ? 512 * 8 : 1];      // only rows of up to 256 threads share a workgroup
-  const int TPR = SUB ? SUB : a.tpr;
-  const int slot = threadIdx.x / TPR, t = threadIdx.x - slot * TPR, RPG = blockDim.x / TPR;
+  const int TPR = SUB ? SUB : a.share.tpr, RPG = a.share.slots;
+  const int slot = row_slot<SUB>(a.share), t = threadIdx.x - slot * TPR;
   const int wpr = TPR / 64, wave0 = slot * wpr, lane16 = threadIdx.x & 15;
   float acc[GAIN ? VPT : 1][8];
 #pragma unroll
@@ -502,7 +509,7 @@ template <class T>
 void run_bwd(RmsBwdArgs a, uint32_t grid, hipStream_t st) {
   const BwdShape s = bwd_shape(a.cols);
   const dim3 nt(s.tpr * s.slots);
-  a.tpr = s.tpr;
+  a.share = row_share(s.tpr, s.slots);
   if (s.tpr == 16) hipLaunchKernelGGL((k_rms_bwd<T, 1, 16, 512, true>), dim3(grid), nt, 0, st, a);
   else if (s.tpr == 32) hipLaunchKernelGGL((k_rms_bwd<T, 1, 32, 512, true>), dim3(grid), nt, 0, st, a);
   else if (s.vpt == 1) hipLaunchKernelGGL((k_rms_bwd<T, 1, 0, 768, true>), dim3(grid), nt, 0, st, a);
