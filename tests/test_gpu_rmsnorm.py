@@ -245,7 +245,7 @@ def check_backward(dy, h, gain, rstd, dh, dx, dgain, eps):
     factors: at most 8 roundings on any term, so 8 2^-24 of the terms' magnitudes; the mean adds
     at most 32 products in a thread, 6 steps over a wave and 16 waves, each of which rounds by
     2^-24 of the sum of magnitudes at most: 64 2^-24 of it; then one rounding to the type.  dgain
-    adds up to 16 rows or rows / 256 in a thread, 8 slots, up to 8 partials and then 64 slices in 6
+    adds up to 16 rows or rows / 256 in a thread, 32 slots, up to 8 partials and then 64 slices in 6
     steps: each addition rounds by 2^-24 of the magnitudes' sum at most, fewer than rows / 256 + 64
     of them one after another."""
     cols = h.shape[-1]
@@ -282,6 +282,16 @@ def test_backward(rows, cols, dtype):
         check_backward(dy, h, gain, rstd, e, dx, dgain, 1e-3)
         again, g2 = F.fp4root_rmsnorm_backward(dy, h, gain, rstd, dh=e)
         assert torch.equal(again, dx) and torch.equal(g2, dgain)
+
+
+@pytest.mark.parametrize("rows,cols", [(2050, 2100), (2049, 4096), (4100, 1500), (2600, 5000), (70000, 40)])
+def test_backward_of_many_rows(rows, cols):
+    """More rows than workgroups, with 2 and 3 workgroups a CU and rows that share one."""
+    h, dy = randn((rows, cols), torch.bfloat16, 61), randn((rows, cols), torch.bfloat16, 62)
+    gain = randn((cols,), torch.float32, 63)
+    rstd = F.fp4root_rmsnorm_quantize(h, gain, quantize=False).rstd
+    dx, dgain = F.fp4root_rmsnorm_backward(dy, h, gain, rstd, dh=h)
+    check_backward(dy, h, gain, rstd, h, dx, dgain, 1e-6)
 
 
 def test_backward_against_differences():

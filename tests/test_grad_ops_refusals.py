@@ -193,3 +193,12 @@ def test_rows_of_refused_views():
     for bad in (t[:, :2, :4], torch.zeros(1, 8).expand(4, 8), torch.zeros(40).as_strided((4, 8), (4, 1))):
         with pytest.raises(ValueError):
             F._as_rows(bad, "t")
+
+
+def test_row_of_a_thread_by_multiplication():
+    """The kernels divide a thread's number by the threads a row takes through 2^20 over them,
+    rounded up, in 32 bits."""
+    for tpr in range(64, 1025, 64):
+        inverse = -(-(1 << 20) // tpr)
+        for t in range(1024):
+            assert (t * inverse) >> 20 == t // tpr and t * inverse < 1 << 32
