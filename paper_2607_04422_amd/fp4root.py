@@ -669,7 +669,10 @@ def fp4root_clip_grads(grads, max_norm: float, outputs=None, norm_type=2, eps: f
     """Clip a list of gradient tensors by their global norm, in place or into `outputs`; returns
     the norm before clipping (a float32 GPU scalar).  A program that clips the same buffers step
     after step keeps a GradClipper instead."""
+    grads = list(grads)
     if stream is not None:        # allocated where it is used
+        if grads:
+            _launch_stream(grads[0].device, stream)
         with torch.cuda.stream(stream):
             return fp4root_clip_grads(grads, max_norm, outputs, norm_type, eps)
     c = GradClipper.__new__(GradClipper)
@@ -748,6 +751,7 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     (h may be the residual or x itself: in place); status: an int32 GPU tensor of one element.
     See fp4root_rmsnorm_quantize in include/fp4root.h."""
     if stream is not None:        # allocated where it is used
+        _launch_stream(x.device, stream)
         with torch.cuda.stream(stream):
             return fp4root_rmsnorm_quantize(x, gain, residual, eps, group, e8m0, quantize, want_y, out, status)
     type_ = _need_stream(x, "x")
@@ -755,8 +759,11 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     rows, ld_x = _matrix(x, "x")
     shape, dev = x.shape, x.device
     lead, cols = shape[:-1], shape[-1]
-    ld_r = _matrix(residual, "residual", x)[1] if residual is not None else 0
-    raw = _launch_stream(dev, None)
+    ld_r = ld_h = ld_y = 0
+    x_p, gain_p = x.data_ptr(), gain.data_ptr() if gain is not None else None
+    r_p = h_p = y_p = codes_p = scales_p = rstd_p = status_p = None
+    if residual is not None:
+        ld_r, r_p = _matrix(residual, "residual", x)[1], residual.data_ptr()
     if out is None:
         # empty_like keeps a stride, and is the cheaper call
         packed = ld_x == cols and x.is_contiguous()
@@ -769,9 +776,9 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
             x.new_empty(lead, dtype=torch.float32)
         h = x if residual is None else torch.empty_like(x) if packed else x.new_empty(shape)
         if want_y:
-            y = x.new_empty(shape)
+            y, ld_y = x.new_empty(shape), cols
+        ld_h = cols
         out = RmsNormOutput(codes, scales, rstd, h, y)
-        ld_h = ld_y = cols
     else:
         codes, scales, rstd, h, y = out
         for name, t, dtype, want in (("codes", codes, torch.uint8, shape),
@@ -783,17 +790,28 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
                 raise ValueError(f"out.{name} must be a contiguous {dtype} tensor of shape {tuple(want)} on x's GPU")
         if residual is None and h is not x:
             out = out._replace(h=x)        # the stream is x: nothing to write
-        ld_h = _matrix(h, "out.h", x)[1] if residual is not None and h is not None else 0
-        ld_y = _matrix(y, "out.y", x)[1] if y is not None else 0
-    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.device != dev):
-        raise ValueError("status must be one int32 element on x's GPU")
-    a = RmsNorm(x.data_ptr(), residual.data_ptr() if residual is not None else None, gain.data_ptr() if gain is not None else None,
-                h.data_ptr() if residual is not None and h is not None else None,
-                y.data_ptr() if y is not None else None, codes.data_ptr() if codes is not None else None,
-                scales.data_ptr() if scales is not None else None, rstd.data_ptr() if rstd is not None else None,
-                status.data_ptr() if status is not None else None, rows, cols, ld_x, ld_r, ld_h, ld_y, type_,
-                gain_type, group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps)
-    _check(_call(_lib.fp4root_rmsnorm_quantize, dev, ctypes.byref(a), raw), "fp4root_rmsnorm_quantize")
+        if residual is not None and h is not None:
+            ld_h = _matrix(h, "out.h", x)[1]
+        if y is not None:
+            ld_y = _matrix(y, "out.y", x)[1]
+    if residual is not None and h is not None:
+        h_p = h.data_ptr()
+    if y is not None:
+        y_p = y.data_ptr()
+    if codes is not None:
+        codes_p = codes.data_ptr()
+    if scales is not None:
+        scales_p = scales.data_ptr()
+    if rstd is not None:
+        rstd_p = rstd.data_ptr()
+    if status is not None:
+        if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
+            raise ValueError("status must be one int32 element on x's GPU")
+        status_p = status.data_ptr()
+    a = RmsNorm(x_p, r_p, gain_p, h_p, y_p, codes_p, scales_p, rstd_p, status_p, rows, cols, ld_x, ld_r, ld_h, ld_y,
+                type_, gain_type, group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps)
+    _check(_call(_lib.fp4root_rmsnorm_quantize, dev, ctypes.byref(a), _launch_stream(dev, None)),
+           "fp4root_rmsnorm_quantize")
     return out
 
 
@@ -804,6 +822,7 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     h's type is the gradient of x and of the residual alike, dgain is float32.  dx may be given
     (dy, h or dh itself: in place); see fp4root_rmsnorm_backward in include/fp4root.h."""
     if stream is not None:        # allocated where it is used
+        _launch_stream(h.device, stream)
         with torch.cuda.stream(stream):
             return fp4root_rmsnorm_backward(dy, h, gain, rstd, dh, dx, dgain, want_dgain, ws)
     type_ = _need_stream(h, "h")
@@ -815,29 +834,29 @@ def fp4root_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: Optional[t
     _need_gpu_f32(rstd, "rstd")
     if rstd.numel() != rows or not rstd.is_contiguous() or rstd.device != dev:
         raise ValueError("rstd must hold one contiguous element per row on h's GPU")
-    raw = _launch_stream(dev, None)
     if dx is None:
         dx = torch.empty_like(h) if ld_h == cols and h.is_contiguous() else h.new_empty(h.shape)
         ld_dx = cols
     else:
         ld_dx = _matrix(dx, "dx", h)[1]
-    need = 0
-    if dgain is None and want_dgain:
-        dgain = h.new_empty(cols, dtype=torch.float32)
     if dgain is not None:
         _need_gpu_f32(dgain, "dgain")
         if dgain.numel() != cols or not dgain.is_contiguous() or dgain.device != dev:
             raise ValueError("dgain must hold one contiguous element per column on h's GPU")
-        need = _lib.fp4root_rmsnorm_backward_workspace(rows, cols)
+    elif want_dgain:
+        dgain = h.new_empty(cols, dtype=torch.float32)
+    dgain_p = ws_p = None
+    ws_bytes = 0
+    if dgain is not None:
         if ws is None:
-            ws = h.new_empty(need, dtype=torch.uint8)
+            ws = h.new_empty(_lib.fp4root_rmsnorm_backward_workspace(rows, cols), dtype=torch.uint8)
         elif ws.device != dev or not ws.is_contiguous():
             raise ValueError("ws must be contiguous on h's GPU")
+        dgain_p, ws_p, ws_bytes = dgain.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size()
     _check(_call(_lib.fp4root_rmsnorm_backward, dev, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h,
                  dh.data_ptr() if dh is not None else None, ld_dh, gain.data_ptr() if gain is not None else None,
-                 rstd.data_ptr(), dx.data_ptr(), ld_dx, dgain.data_ptr() if dgain is not None else None, rows, cols,
-                 type_, gain_type, ws.data_ptr() if need else None,
-                 ws.numel() * ws.element_size() if need else 0, raw), "fp4root_rmsnorm_backward")
+                 rstd.data_ptr(), dx.data_ptr(), ld_dx, dgain_p, rows, cols, type_, gain_type, ws_p, ws_bytes,
+                 _launch_stream(dev, None)), "fp4root_rmsnorm_backward")
     return dx, dgain
 
 

@@ -202,3 +202,11 @@ def test_row_of_a_thread_by_multiplication():
         inverse = -(-(1 << 20) // tpr)
         for t in range(1024):
             assert (t * inverse) >> 20 == t // tpr and t * inverse < 1 << 32
+
+
+def test_a_stream_of_another_gpu_is_refused():
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 7
+    assert F._launch_stream(torch.device("cuda", 1), Stream()) == 7
+    with pytest.raises(ValueError):
+        F._launch_stream(torch.device("cuda", 0), Stream())
