@@ -357,8 +357,8 @@ typedef struct {
 /* Device bytes of a list of `count` tensors (host array, at most 2^20), or 0 for an invalid one. */
 size_t fp4root_grad_list_size(const fp4root_tensor* tensors, int64_t count);
 
-/* Writes the table into `mem` (mem_bytes >= the size above, 256-byte aligned) and the handle
- * into *list.  Asynchronous: calls on another stream have to wait for it.  An output that is
+/* Writes the table (and a status of 0) into `mem` (mem_bytes >= the size above, 256-byte aligned)
+ * and the handle into *list.  Asynchronous: calls on another stream have to wait for it.  An output that is
  * not its own input but meets it or another tensor of the list, and a tensor written twice, are
  * refused (FP4ROOT_ERR_INVALID_ARG). */
 int fp4root_grad_list_init(fp4root_grad_list* list, const fp4root_tensor* tensors, int64_t count, void* mem,

@@ -143,7 +143,10 @@ FP4R_DEV double part_value(const GradRef& t, int64_t v0, int64_t v1) {
 __global__ __launch_bounds__(kThreads) void k_grad_table(GradChunk ch, GradTable tb, uint32_t first_tensor) {
   const int i = blockIdx.x;
   const uint32_t t = first_tensor + i;
-  if (threadIdx.x == 0) tb.tensors[t] = ch.t[i];
+  if (threadIdx.x == 0) {
+    tb.tensors[t] = ch.t[i];
+    if (t == 0) *tb.status = 0u;
+  }
   for (uint32_t p = threadIdx.x; p < ch.parts[i]; p += kThreads) tb.parts[ch.t[i].first + p] = GradPart{t, p};
 }
 

@@ -80,6 +80,7 @@ def test_norm_and_clip(name, dtype, kind):
     for max_norm in (1e-2, 1e6, math.inf):
         outs = [torch.full_like(g, 7.0, dtype=torch.float32) for g in grads]
         c = F.GradClipper(grads, max_norm, outputs=outs, norm_type=kind)
+        assert c.status() == 0 and float(c.total) == 0.0
         c()
         check(c, grads, kind)
         for g, o in zip(grads, outs):
