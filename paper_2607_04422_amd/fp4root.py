@@ -755,29 +755,32 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
         with torch.cuda.stream(stream):
             return fp4root_rmsnorm_quantize(x, gain, residual, eps, group, e8m0, quantize, want_y, out, status)
     type_ = _need_stream(x, "x")
-    gain_type = _gain_type(gain, x)
-    rows, ld_x = _matrix(x, "x")
-    shape, dev = x.shape, x.device
+    shape, dev, packed = x.shape, x.device, x.is_contiguous()
     lead, cols = shape[:-1], shape[-1]
-    ld_r = ld_h = ld_y = 0
-    x_p, gain_p = x.data_ptr(), gain.data_ptr() if gain is not None else None
-    r_p = h_p = y_p = codes_p = scales_p = rstd_p = status_p = None
+    rows, ld_x = (x.numel() // cols, cols) if packed and cols else _matrix(x, "x")
+    gain_type = ld_r = ld_h = ld_y = 0
+    gain_p = r_p = h_p = y_p = codes_p = scales_p = rstd_p = status_p = None
+    if gain is not None:
+        gain_type, gain_p = _gain_type(gain, x), gain.data_ptr()
     if residual is not None:
         ld_r, r_p = _matrix(residual, "residual", x)[1], residual.data_ptr()
     if out is None:
         # empty_like keeps a stride, and is the cheaper call
-        packed = ld_x == cols and x.is_contiguous()
         codes = scales = y = None
         if quantize:
             codes = torch.empty_like(x, dtype=torch.uint8) if packed else x.new_empty(shape, dtype=torch.uint8)
             scales = x.new_empty((*lead, -(-cols // group)) if group > 0 else lead,
                                  dtype=torch.uint8 if e8m0 else torch.float32)
+            codes_p, scales_p = codes.data_ptr(), scales.data_ptr()
         rstd = torch.empty_like(scales) if quantize and group == 0 and not e8m0 else \
             x.new_empty(lead, dtype=torch.float32)
-        h = x if residual is None else torch.empty_like(x) if packed else x.new_empty(shape)
+        rstd_p, h = rstd.data_ptr(), x
+        if residual is not None:
+            h, ld_h = torch.empty_like(x) if packed else x.new_empty(shape), cols
+            h_p = h.data_ptr()
         if want_y:
             y, ld_y = x.new_empty(shape), cols
-        ld_h = cols
+            y_p = y.data_ptr()
         out = RmsNormOutput(codes, scales, rstd, h, y)
     else:
         codes, scales, rstd, h, y = out
@@ -791,24 +794,15 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
         if residual is None and h is not x:
             out = out._replace(h=x)        # the stream is x: nothing to write
         if residual is not None and h is not None:
-            ld_h = _matrix(h, "out.h", x)[1]
+            ld_h, h_p = _matrix(h, "out.h", x)[1], h.data_ptr()
         if y is not None:
-            ld_y = _matrix(y, "out.y", x)[1]
-    if residual is not None and h is not None:
-        h_p = h.data_ptr()
-    if y is not None:
-        y_p = y.data_ptr()
-    if codes is not None:
-        codes_p = codes.data_ptr()
-    if scales is not None:
-        scales_p = scales.data_ptr()
-    if rstd is not None:
-        rstd_p = rstd.data_ptr()
+            ld_y, y_p = _matrix(y, "out.y", x)[1], y.data_ptr()
+        codes_p, scales_p, rstd_p = (t.data_ptr() if t is not None else None for t in (codes, scales, rstd))
     if status is not None:
         if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
             raise ValueError("status must be one int32 element on x's GPU")
         status_p = status.data_ptr()
-    a = RmsNorm(x_p, r_p, gain_p, h_p, y_p, codes_p, scales_p, rstd_p, status_p, rows, cols, ld_x, ld_r, ld_h, ld_y,
+    a = RmsNorm(x.data_ptr(), r_p, gain_p, h_p, y_p, codes_p, scales_p, rstd_p, status_p, rows, cols, ld_x, ld_r, ld_h, ld_y,
                 type_, gain_type, group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps)
     _check(_call(_lib.fp4root_rmsnorm_quantize, dev, ctypes.byref(a), _launch_stream(dev, None)),
            "fp4root_rmsnorm_quantize")
