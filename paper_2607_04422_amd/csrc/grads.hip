@@ -274,8 +274,8 @@ hipError_t launch_grad_table(const GradChunk& ch, const GradTable& tb, uint32_t 
 }
 
 template <bool MAX>
-static void grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool past, double max_norm, double eps, double* total,
-                      float* norms, float* result, hipStream_t st) {
+static void grad_norm(const GradTable& tb, uint32_t count, uint32_t parts, bool past, double max_norm, double eps,
+                      double* total, float* norms, float* result, hipStream_t st) {
   if (parts) {
     if (past) hipLaunchKernelGGL((k_grad_parts<MAX, true>), dim3(parts), dim3(kThreads), 0, st, tb);
     else hipLaunchKernelGGL((k_grad_parts<MAX, false>), dim3(parts), dim3(kThreads), 0, st, tb);

@@ -603,7 +603,8 @@ class GradClipper:
             ld_out = ld
             if o is not g:
                 rows, cols, ld, ld_out = _rows_of_both(g, o, rows, cols, ld, i)
-            tensors[i] = Tensor(g.data_ptr(), None if measure_only else o.data_ptr(), rows, cols, ld, ld_out, _TYPES[g.dtype], _TYPES[o.dtype])
+            tensors[i] = Tensor(g.data_ptr(), None if measure_only else o.data_ptr(), rows, cols, ld, ld_out,
+                                _TYPES[g.dtype], _TYPES[o.dtype])
         self.device = self.grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
         need = lib.fp4root_grad_list_size(tensors, n)
         if need == 0:
@@ -802,8 +803,8 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
         if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
             raise ValueError("status must be one int32 element on x's GPU")
         status_p = status.data_ptr()
-    a = RmsNorm(x.data_ptr(), r_p, gain_p, h_p, y_p, codes_p, scales_p, rstd_p, status_p, rows, cols, ld_x, ld_r, ld_h, ld_y,
-                type_, gain_type, group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps)
+    a = RmsNorm(x.data_ptr(), r_p, gain_p, h_p, y_p, codes_p, scales_p, rstd_p, status_p, rows, cols, ld_x, ld_r,
+                ld_h, ld_y, type_, gain_type, group, SCALE_E8M0 if e8m0 else SCALE_FP32, eps)
     _check(_call(_lib.fp4root_rmsnorm_quantize, dev, ctypes.byref(a), _launch_stream(dev, None)),
            "fp4root_rmsnorm_quantize")
     return out
