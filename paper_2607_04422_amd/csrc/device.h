@@ -476,10 +476,20 @@ FP4R_DEV float fast_sqrt(float v) {
 FP4R_DEV float fast_div(float a, double rb) { return (float)((double)a * rb); }
 
 // 1 / b in binary64, within 2^-52: the residual e of rcp(b) is below 2^-22, so
-// x (1 + e + e^2) leaves 2^-66 and two roundings.
+// x (1 + e + e^2) leaves 2^-66 and two roundings.  For b up to 2^126: past it the estimate is
+// subnormal and the instruction gives 0.
 FP4R_DEV double recip64(float b) {
   const double x = (double)__builtin_amdgcn_rcpf(b), e = __builtin_fma(-(double)b, x, 1.0);
   return __builtin_fma(x, __builtin_fma(e, e, e), x);
+}
+
+// The scale amax / 448 of a group of E4M3 codes, and what its values are multiplied by,
+// fl32(448 / amax), for amax in [2^-100, FLT_MAX].  As above, amax / 448 is at least 2^-28 from
+// every midpoint and 448 / amax 2^-49; large values are scaled by 2^-64, which is exact.
+FP4R_DEV float scale_448(float amax) { return (float)((double)amax * (1.0 / 448.0)); }
+FP4R_DEV float inverse_448(float amax) {
+  const bool large = amax >= 0x1p64f;
+  return (float)((large ? 448.0 * 0x1p-64 : 448.0) * recip64(large ? amax * 0x1p-64f : amax));
 }
 
 // Gradients times the clipping coefficient, where there is one (uniform).

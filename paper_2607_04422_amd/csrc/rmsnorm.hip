@@ -20,7 +20,6 @@
 namespace fp4r {
 namespace {
 
-constexpr float kE4M3Max = 448.0f;
 constexpr float kAmaxMin = 0x1p-100f;
 
 // Lanes l and l ^ 1, l ^ 2 of a quad, then the other quad of 8 lanes, the other half of 16.
@@ -89,8 +88,8 @@ FP4R_DEV float scale_of(float amax, int e8m0, uint32_t& stored) {
     stored = e;
     return __uint_as_float((254u - e) << 23);
   }
-  stored = __float_as_uint((float)((double)amax * (1.0 / 448.0)));
-  return (float)(448.0 * recip64(amax));
+  stored = __float_as_uint(scale_448(amax));
+  return inverse_448(amax);
 }
 FP4R_DEV void store_scale(const RmsArgs& a, int64_t i, uint32_t stored) {
   if (a.e8m0) reinterpret_cast<uint8_t*>(a.scales)[i] = (uint8_t)stored;

@@ -61,6 +61,21 @@ __global__ __launch_bounds__(256) void k_div(uint64_t seed, uint32_t count, uint
   }
   report(out, bad, which);
 }
+
+// The scale and the inverse scale of a group of E4M3 codes.
+__global__ __launch_bounds__(256) void k_448(uint32_t first, uint32_t count, uint32_t* out) {
+  uint32_t bad = 0, which = 0;
+  for (uint64_t i = blockIdx.x * 256u + threadIdx.x; i < count; i += kBlocks * 256u) {
+    const uint32_t bits = first + (uint32_t)i;
+    const float v = __uint_as_float(bits);
+    if (__float_as_uint(scale_448(v)) != __float_as_uint((float)((double)v / 448.0)) ||
+        __float_as_uint(inverse_448(v)) != __float_as_uint((float)(448.0 / (double)v))) {
+      ++bad;
+      which = bits;
+    }
+  }
+  report(out, bad, which);
+}
 }  // namespace
 
 extern "C" {
@@ -70,6 +85,10 @@ int fp4root_sweep_sqrt(uint32_t first, uint32_t count, uint32_t* out, void* stre
 }
 int fp4root_sweep_bf16(uint32_t first, uint32_t count, uint32_t* out, void* stream) {
   hipLaunchKernelGGL(k_bf16, dim3(kBlocks), dim3(256), 0, (hipStream_t)stream, first, count, out);
+  return (int)hipGetLastError();
+}
+int fp4root_sweep_448(uint32_t first, uint32_t count, uint32_t* out, void* stream) {
+  hipLaunchKernelGGL(k_448, dim3(kBlocks), dim3(256), 0, (hipStream_t)stream, first, count, out);
   return (int)hipGetLastError();
 }
 int fp4root_sweep_div(uint64_t seed, uint32_t count, uint32_t* out, void* stream) {
