@@ -693,6 +693,16 @@ class RmsNormOutput(NamedTuple):
     y: Optional[torch.Tensor]
 
 
+class _Unadded(RmsNormOutput):
+    """The result of a call without a residual: its h is the caller's x and no output, unless the
+    caller makes another tensor h."""
+    __slots__ = ()
+
+    def _replace(self, **fields):
+        got = super()._replace(**fields)
+        return RmsNormOutput(*got) if "h" in fields else got
+
+
 def _matrix(t: torch.Tensor, name: str, like: torch.Tensor = None):
     """(rows, row stride) of a tensor whose last dimension is contiguous and whose others are
     rows of one stride; checked against `like`, an accepted one, for type, shape and GPU."""
@@ -749,7 +759,8 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
     """h = x + residual, then its root-mean-square norm times gain, in E4M3 with a scale per row
     (group 0) or per group of 32, 64 or 128 columns.  x: (..., cols), float32, bfloat16 or
     float16, rows of one stride; out: an earlier call's result, whose tensors are written again
-    (h may be the residual or x itself: in place); status: an int32 GPU tensor of one element.
+    (out._replace(h=...) with the residual or x itself: in place), but for the h of a call without a
+    residual, which is that call's x and is replaced; status: an int32 GPU tensor of one element.
     See fp4root_rmsnorm_quantize in include/fp4root.h."""
     if stream is not None:        # allocated where it is used
         _launch_stream(x.device, stream)
@@ -782,7 +793,7 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
         if want_y:
             y, ld_y = x.new_empty(shape), cols
             y_p = y.data_ptr()
-        out = RmsNormOutput(codes, scales, rstd, h, y)
+        out = (RmsNormOutput if residual is not None else _Unadded)(codes, scales, rstd, h, y)
     else:
         codes, scales, rstd, h, y = out
         for name, t, dtype, want in (("codes", codes, torch.uint8, shape),
@@ -792,8 +803,11 @@ def fp4root_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor = None, residua
             if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(want) or not t.is_contiguous() or
                                   t.device != dev):
                 raise ValueError(f"out.{name} must be a contiguous {dtype} tensor of shape {tuple(want)} on x's GPU")
-        if residual is None and h is not x:
-            out = out._replace(h=x)        # the stream is x: nothing to write
+        if residual is None:
+            out = _Unadded(codes, scales, rstd, x, y)      # the stream is x: nothing to write
+        elif type(out) is _Unadded:
+            h = torch.empty_like(x) if packed else x.new_empty(shape)
+            out = RmsNormOutput(codes, scales, rstd, h, y)
         if residual is not None and h is not None:
             ld_h, h_p = _matrix(h, "out.h", x)[1], h.data_ptr()
         if y is not None:
