@@ -426,9 +426,9 @@ typedef struct {
   uint8_t* codes;        /* rows x cols E4M3FN codes, contiguous, or NULL (then scales too)   */
   void* scales;          /* rows x ceil(cols / group) (one a row for group 0), contiguous     */
   float* rstd;           /* rows, for the backward pass, or NULL                              */
-  int32_t* status;       /* set to FP4ROOT_ERR_NONFINITE where a row of x + residual or a group
-                            of outputs holds an infinity, or such a row a NaN, and left as it
-                            is otherwise; or NULL                                             */
+  int32_t* status;       /* set to FP4ROOT_ERR_NONFINITE where a row of x + residual, or a group
+                            of the values that are quantized, holds an infinity or a NaN, and
+                            left as it is otherwise; or NULL                                  */
   int64_t rows, cols;    /* rows >= 0; cols in [1, 32768]                                     */
   int64_t ld_x, ld_residual, ld_h, ld_y;
   int32_t type;          /* FP4ROOT_FLOAT32, FP4ROOT_BFLOAT16 or FP4ROOT_FLOAT16              */
@@ -443,7 +443,9 @@ typedef struct {
  * with the sum and the root in binary64, y = fl32(fl32(h rstd) gain), amax = max(max |y|,
  * 2^-100) over a row or group, code = E4M3(fl32(y / s)) round to nearest even, with 1 / s as
  * fl32(448 / amax) for FP32 scales and exact for E8M0.  A value is code * s.  A row with a NaN
- * or an infinity in h has rstd and codes NaN; other rows are not touched by it. */
+ * or an infinity in h has rstd and codes NaN; other rows are not touched by it.  A group with a
+ * NaN or an infinity in y (of the gain) has codes NaN and a scale that is not finite (E8M0: 255,
+ * its NaN); other groups are not touched by it. */
 int fp4root_rmsnorm_quantize(const fp4root_rmsnorm* args, void* stream);
 
 /* Workspace bytes fp4root_rmsnorm_backward needs, or 0 for a bad shape. */

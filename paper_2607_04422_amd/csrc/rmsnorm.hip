@@ -22,16 +22,19 @@ namespace {
 
 constexpr float kAmaxMin = 0x1p-100f;
 
+// The larger of two magnitudes, NaN if either is (one instruction takes three).
+FP4R_DEV float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // Lanes l and l ^ 1, l ^ 2 of a quad, then the other quad of 8 lanes, the other half of 16.
 template <int CTRL>
 FP4R_DEV float dpp_f(float v) {
   return __uint_as_float(dpp_u<CTRL>(__float_as_uint(v)));
 }
 FP4R_DEV float group_max(float v, int lanes) {   // lanes: 4, 8 or 16 (uniform)
-  v = fmaxf(v, dpp_f<0xB1>(v));
-  v = fmaxf(v, dpp_f<0x4E>(v));
-  if (lanes > 4) v = fmaxf(v, dpp_f<0x141>(v));
-  if (lanes > 8) v = fmaxf(v, dpp_f<0x140>(v));
+  v = larger(v, dpp_f<0xB1>(v));
+  v = larger(v, dpp_f<0x4E>(v));
+  if (lanes > 4) v = larger(v, dpp_f<0x141>(v));
+  if (lanes > 8) v = larger(v, dpp_f<0x140>(v));
   return v;
 }
 FP4R_DEV float lane_f(float v, int lane) {
@@ -39,7 +42,7 @@ FP4R_DEV float lane_f(float v, int lane) {
 }
 FP4R_DEV float wave_max(float v) {
   v = group_max(v, 16);
-  return fmaxf(fmaxf(lane_f(v, 0), lane_f(v, 16)), fmaxf(lane_f(v, 32), lane_f(v, 48)));
+  return larger(larger(lane_f(v, 0), lane_f(v, 16)), larger(lane_f(v, 32), lane_f(v, 48)));
 }
 // Sums over the lanes of a row: SUB lanes (16 or 32), or the wave for SUB 0.
 template <int SUB>
@@ -65,7 +68,7 @@ template <int SUB>
 FP4R_DEV float lanes_max(float v) {
   if constexpr (SUB == 0) return wave_max(v);
   v = group_max(v, 16);
-  return SUB == 16 ? v : fmaxf(v, __shfl_xor(v, 16));
+  return SUB == 16 ? v : larger(v, __shfl_xor(v, 16));
 }
 
 // 1 / sqrt(a) for 0 < a < 2^1000: the instruction's estimate and two Newton steps.
@@ -79,14 +82,16 @@ FP4R_DEV double rsqrt64(double a) {
   return r;
 }
 
-// The scale of a group as it is stored, and what its values are multiplied by.
+// The scale of a group as it is stored, and what its values are multiplied by: NaN where the
+// largest is an infinity or NaN, so that no finite value of the group passes for 0.
 FP4R_DEV float scale_of(float amax, int e8m0, uint32_t& stored) {
-  amax = fmaxf(amax, kAmaxMin);
+  amax = larger(amax, kAmaxMin);
   if (e8m0) {
-    // amax = 1.m 2^(e - 127) and 448 = 1.75 2^8
+    // amax = 1.m 2^(e - 127) and 448 = 1.75 2^8; E8M0 holds NaN as 255
     const uint32_t b = __float_as_uint(amax), e = (b >> 23) - 8u + ((b & 0x7FFFFFu) > 0x600000u);
-    stored = e;
-    return __uint_as_float((254u - e) << 23);
+    const bool finite = b < 0x7F800000u;
+    stored = finite ? e : 255u;
+    return __uint_as_float(finite ? (254u - e) << 23 : 0x7FC00000u);
   }
   stored = __float_as_uint(scale_448(amax));
   return inverse_448(amax);
@@ -231,7 +236,7 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(RmsArgs a) {
     if (!a.codes) continue;
     float m = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf(y[k]));
+    for (int k = 0; k < 8; ++k) m = larger(m, fabsf(y[k]));
     if (lanes) {
       m = group_max(m, lanes);
       uint32_t stored;
@@ -242,7 +247,7 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(RmsArgs a) {
         if (a.status && !(m < __builtin_inff())) *a.status = kErrNonFinite;
       }
     }
-    top = fmaxf(top, m);
+    top = larger(top, m);
   }
   if (!a.codes || lanes) return;
   top = lanes_max<SUB>(top);
