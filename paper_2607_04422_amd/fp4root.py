@@ -569,8 +569,10 @@ class GradClipper:
     (it counts twice).  RootStep, fp4root_qadamw_update and fp4root_momentum_update take `coef` as
     grad_scale and then need no scaled gradients.  Each may be captured into a HIP graph, and
     used on any stream once the object is made (it waits for its own set-up); calls of one
-    GradClipper on two streams at once race.  The gradients' memory must stay where it is, and the
-    object alive, until its calls have run.
+    GradClipper on two streams at once race.  It reads the tensors it was made with: a gradient that
+    a later step puts into a new tensor (a `.grad` set to None in between, a dgain that
+    fp4root_rmsnorm_backward allocates) is not seen, so give such producers their buffer.  The
+    gradients' memory must stay where it is, and the object alive, until its calls have run.
     """
 
     def __init__(self, grads, max_norm: float, outputs=None, norm_type=2, eps: float = 1e-6,
