@@ -455,11 +455,13 @@ __global__ __launch_bounds__(256) void k_rms_cols(RmsBwdArgs a, int64_t chunk) {
 }
 
 // 16 columns by 64 slices of the partial rows a workgroup: each thread adds four columns of
-// every 64th row, eight loads in flight, then the slices in pairs.
+// every 64th row, eight loads in flight, then the slices in pairs.  In binary64, so that what
+// workgroups of opposite sign cancel is not lost: the partials are binary32 sums of the rows of one
+// workgroup, and the join adds one rounding.
 __global__ __launch_bounds__(256) void k_rms_dgain(const float* partial, int count, int cols, float* dgain) {
-  __shared__ float red[16][65];
+  __shared__ double red[16][65];
   const int q = threadIdx.x & 3, slice = threadIdx.x >> 2, c = blockIdx.x * 16 + q * 4, n = min(4, cols - c);
-  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
   if (n > 0) {
     for (int p = slice; p < count; p += 64 * 8) {
       float x[8][4];
@@ -468,7 +470,7 @@ __global__ __launch_bounds__(256) void k_rms_dgain(const float* partial, int cou
 #pragma unroll
       for (int u = 0; u < 8; ++u)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] += p + u * 64 < count ? x[u][k] : 0.0f;
+        for (int k = 0; k < 4; ++k) s[k] += p + u * 64 < count ? (double)x[u][k] : 0.0;
     }
   }
 #pragma unroll
@@ -476,10 +478,10 @@ __global__ __launch_bounds__(256) void k_rms_dgain(const float* partial, int cou
   __syncthreads();
   // 16 threads a column
   const int col = threadIdx.x >> 4, l = threadIdx.x & 15;
-  float v = (red[col][l] + red[col][l + 16]) + (red[col][l + 32] + red[col][l + 48]);
+  double v = (red[col][l] + red[col][l + 16]) + (red[col][l + 32] + red[col][l + 48]);
 #pragma unroll
   for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o);
-  if (l == 0 && blockIdx.x * 16 + col < cols) dgain[blockIdx.x * 16 + col] = v;
+  if (l == 0 && blockIdx.x * 16 + col < cols) dgain[blockIdx.x * 16 + col] = (float)v;
 }
 
 // Threads a row, vectors a thread and rows a workgroup.  A thread keeps 8 columns where 768
