@@ -1514,7 +1514,10 @@ size_t carve_grad_list(void* base, int64_t count, int64_t parts, GradTable& w) {
 // 12.4 us clipped, 15.2 past them).  A larger one does not, and its loads run faster past them:
 // the norm of 2.8 GB 467 -> 415 us, of 227 MB 45 -> 39.  The norm of a list with outputs elsewhere
 // stays in, since its second pass then finds more in the last-level cache (354 M BF16 elements
-// into FP32: 487 us, and 510 with both past it; in place, 192 MB: 68 and 65).
+// into FP32: 487 us, and 510 with both past it).  That holds in place too where the list is
+// clipped (402 MB of FP32: 191 us, 215 with the norm past it; 2.9 GB: 1539 and 1526), but a list
+// under max_norm costs its norm alone, since the coefficient 1 leaves it as it is (402 MB: 73 us
+// in, 64 past), so in place the norm goes past.
 enum { kListOutputs = 1, kListNormPast = 2, kListScalePast = 4 };
 constexpr int64_t kCachedBytes = int64_t(32) << 20;
 int32_t list_flags(const fp4root_tensor* t, int64_t count, bool out) {
