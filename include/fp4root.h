@@ -372,25 +372,26 @@ int fp4root_grad_list_init(fp4root_grad_list* list, const fp4root_tensor* tensor
  *   result: device floats: result[0] = the norm, result[1] = the clipping coefficient
  *           min(1, max_norm / (norm + eps)), formed in binary64 and rounded once.
  * Squares are exact in binary64 and summed there in an order that depends on each tensor's
- * size alone, so nothing overflows, a tensor's norm does not change with the tensors beside it
- * and repeated calls give the same bits.  A NaN makes the norms it enters and the coefficient
+ * type, shape and strides (and its output's strides) alone, so nothing overflows, a tensor's norm
+ * does not change with the tensors beside it and repeated calls give the same bits.  A NaN makes the norms it enters and the coefficient
  * NaN; an infinity makes the norms infinite and the coefficient 0 (NaN where max_norm is
  * infinite too); both are reported by fp4root_device_status(list->mem).  Calls on one list that
  * overlap in time race. */
 int fp4root_grad_norm(const fp4root_grad_list* list, int kind, double max_norm, double eps, double* total,
                       float* norms, float* result, void* stream);
 
-/* result (as above) from a total on the device. */
+/* result (as above) from a total on the device.  No list's status changes: of ranks that add
+ * their totals, one whose own shard is finite has a status of 0 beside a norm that is not. */
 int fp4root_clip_coef(const double* total, int kind, double max_norm, double eps, float* result, void* stream);
 
 /* out = round(fl32(in * *coef)) for every tensor of a list with outputs, coef a device float
- * (result + 1 above).  Tensors in place that the coefficient 1 leaves as they are, are not
+ * (result + 1 above) in none of them.  Tensors in place that the coefficient 1 leaves as they are, are not
  * touched.  A result past the output type's largest becomes an infinity. */
 int fp4root_clip_grads(const fp4root_grad_list* list, const float* coef, void* stream);
 
 /* fp4root_momentum_update, fp4root_qadamw_update and fp4root_root_step with every gradient
- * element g replaced by fl32(g * *grad_scale), grad_scale a device float: clipping without
- * another pass over the gradients.  The same bits as after fp4root_clip_grads in place;
+ * element g replaced by fl32(g * *grad_scale), grad_scale a device float that the call does not
+ * write: clipping without another pass over the gradients.  The same bits as after fp4root_clip_grads in place;
  * NULL: the gradients as they are. */
 int fp4root_momentum_update_scaled(const float* g, float* m, int64_t batch, int64_t rows, int64_t cols,
                                    uint8_t* codes, uint8_t* scales, float* tensor_scale, float beta,
@@ -454,8 +455,10 @@ size_t fp4root_rmsnorm_backward_workspace(int64_t rows, int64_t cols);
 /* Gradients of y = (h rstd) gain (the rounding to 8 bits passed through as it is):
  *   g = dy gain, xhat = h rstd, dx = rstd (g - xhat mean(g xhat)) + dh,
  *   dgain = sum over rows of dy xhat.
- * dx is the gradient of x and of the residual alike, rounded once; dgain is FP32 (what
- * fp4root_qadamw_update reads) and its sum's order depends on the shape alone.  A row whose rstd
+ * dx is the gradient of x and of the residual alike, formed in binary32 (the mean a binary32 sum
+ * times fl32(1 / cols)) and rounded to the type at the end; dgain is FP32 (what
+ * fp4root_qadamw_update reads): binary32 sums of the products of a workgroup's rows, joined in
+ * binary64, in an order that depends on the shape alone.  A row whose rstd
  * is NaN has a dx of NaN, and makes dgain NaN.
  *   dy, h, dh (gradient that reaches h past the norm, or NULL), dx: rows x cols of `type`, row
  *   strides ld_*; dx may be dy, h or dh; rstd: rows floats; gain: cols, or NULL for ones;

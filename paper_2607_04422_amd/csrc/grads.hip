@@ -6,7 +6,8 @@
 // square is exact, and added there: no overflow and no rounding that matters), one more for
 // the clipping.  Both are bound by memory.
 //
-// A tensor is cut into parts of 16-byte vectors by its own size alone; a workgroup takes one
+// A tensor is cut into parts of 16-byte vectors by its own type, shape and strides (its
+// output's too: beside strided rows a contiguous tensor is walked as rows); a workgroup takes one
 // part, found in a table that the list was given when it was made, so that any number of
 // tensors share a launch.  Every partial result has its own place and the places are added in a
 // fixed order, so a tensor's norm does not change with the tensors beside it and nothing

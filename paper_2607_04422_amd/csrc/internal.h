@@ -427,7 +427,7 @@ hipError_t launch_grad_scale(const GradTable& tb, uint32_t parts, bool past, con
 
 // ---------------------------------------------------------------------------
 // Root-mean-square norm (rmsnorm.hip).
-constexpr int64_t kMaxNormCols = 32768;   // a row stays in the registers of one workgroup
+constexpr int64_t kMaxNormCols = 32768;   // a row stays in one workgroup, 32 columns a thread
 // How the threads of a workgroup share rows (the launch's choice): tpr threads a row, slots rows,
 // and 2^20 / tpr rounded up, which divides a thread's number by tpr (numbers below 1024: its error
 // stays below 2^-10).

@@ -3,10 +3,14 @@
 //   per row, or per group of 32, 64 or 128 columns: amax = max(max |y|, 2^-100),
 //   s = amax / 448, or the smallest power of two with amax <= 448 s;  code = E4M3(y / s)
 // The squares are exact in binary64 and added there, so rstd is the rounding of the exact
-// value but for a few in 2^20 rows, and the scales and codes do not depend on how a row is
-// cut over threads.
+// value but for a few in 2^20 rows: in those its last place, and with it codes and scales, may
+// depend on how the row is cut over threads, which the shape decides.
 //   g = dy gain,  xhat = h rstd,  c = mean(g xhat),  dx = rstd (g - xhat c) + dh,
 //   dgain = sum over rows of dy xhat
+// In the backward pass the row's dot product and a workgroup's part of dgain are binary32 sums: each
+// term is a product of binary32 roundings already, of 16-bit factors for most, and parts of
+// dgain in binary64 would take twice the registers of a thread's columns.  Their join, where
+// hundreds of parts meet, is binary64 (64 x 1024 FP32: error 5.9e-8, 9.5e-8 joined in binary32).
 // Both passes are bound by memory: a row is read once and stays in registers.  A thread holds
 // VPT vectors of 8 columns, as many vectors apart as threads share the row, so a group of columns
 // lies in 4, 8 or 16 adjacent lanes.  A row takes whole waves, or 16 or 32 lanes of one where it
@@ -489,7 +493,9 @@ __global__ __launch_bounds__(256) void k_rms_dgain(const float* partial, int cou
 // 56.0 us, 2 of 256 56.8, 4 of 128 66.8; 8192 x 5120 1 of 640 69.1, 2 of 320 72.3; 8192 x 7168
 // the same; 16384 x 8192 2 of 512 197, 4 of 256 222, 1 of 1024 209), and narrow rows share
 // workgroups of 512 threads (1024: 8192 x 2048 31.0 us for 29.0).  Rows past 16384 columns
-// leave dgain to a pass of its own (with it the registers spill: 4096 x 20000 250 us, so 217).
+// leave dgain to a pass of its own (with it the registers spill: 4096 x 20000 250 us, so 217);
+// past 24576, 1024 threads a row, a thread has 128 registers and a few spill all the same (17 of
+// FP32 rows, 9 of BF16, 2 of FP16: 2048 x 32768 BF16 173 us, FP32 341, 3.1 TB/s).
 struct BwdShape {
   int tpr, vpt, slots;
 };
