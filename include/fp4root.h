@@ -373,10 +373,10 @@ int fp4root_grad_list_init(fp4root_grad_list* list, const fp4root_tensor* tensor
  *           min(1, max_norm / (norm + eps)), formed in binary64 and rounded once.
  * Squares are exact in binary64 and summed there in an order that depends on each tensor's
  * type, shape and strides (and its output's strides) alone, so nothing overflows, a tensor's norm
- * does not change with the tensors beside it and repeated calls give the same bits.  A NaN makes the norms it enters and the coefficient
- * NaN; an infinity makes the norms infinite and the coefficient 0 (NaN where max_norm is
- * infinite too); both are reported by fp4root_device_status(list->mem).  Calls on one list that
- * overlap in time race. */
+ * does not change with the tensors beside it and repeated calls give the same bits.  A NaN makes
+ * the norms it enters and the coefficient NaN; an infinity makes the norms infinite and the
+ * coefficient 0 (NaN where max_norm is infinite too); both are reported by
+ * fp4root_device_status(list->mem).  Calls on one list that overlap in time race. */
 int fp4root_grad_norm(const fp4root_grad_list* list, int kind, double max_norm, double eps, double* total,
                       float* norms, float* result, void* stream);
 

@@ -565,7 +565,8 @@ class GradClipper:
     `norm()` computes these; a call computes them and multiplies every gradient by coef, into
     `outputs` (tensors of the gradients' shapes and any of the types, or None: in place).  Ranks
     that hold shards run `norm()`, all-reduce `total` (sum, or maximum for inf), then `recoef()`
-    and `scale()`; status() goes on to speak of the rank's own shard.  With measure_only there is nothing to scale, and a tensor may be listed twice
+    and `scale()`; status() goes on to speak of the rank's own shard.  With measure_only there is
+    nothing to scale, and a tensor may be listed twice
     (it counts twice).  RootStep, fp4root_qadamw_update and fp4root_momentum_update take `coef` as
     grad_scale and then need no scaled gradients.  Each may be captured into a HIP graph, and
     used on any stream once the object is made (it waits for its own set-up); calls of one

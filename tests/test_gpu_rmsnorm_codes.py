@@ -50,7 +50,8 @@ def check_fp32_scales(x, residual, gain, group, **kw):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("rows,cols,group", [(64, 8192, 0), (37, 5003, 128), (300, 96, 32), (65, 1001, 64), (3, 20000, 0)])
+@pytest.mark.parametrize("rows,cols,group", [(64, 8192, 0), (37, 5003, 128), (300, 96, 32), (65, 1001, 64),
+                                             (3, 20000, 0)])
 def test_codes_and_scales(rows, cols, group, dtype):
     g = gen(rows + cols)
     x = (torch.randn(rows, cols, generator=g, device="cuda") * 3).to(dtype)
@@ -87,7 +88,8 @@ def test_quotients_by_448_every_value():
     torch.cuda.synchronize()
     first = 0x0D800000
     count = 0x7F7FFFFF - first + 1
-    assert lib.fp4root_sweep_448(ctypes.c_uint32(first), ctypes.c_uint32(count), ctypes.c_void_p(out.data_ptr()), None) == 0
+    u, where = ctypes.c_uint32, ctypes.c_void_p(out.data_ptr())
+    assert lib.fp4root_sweep_448(u(first), u(count), where, None) == 0
     torch.cuda.synchronize()
     bad, which = (int(v) & 0xFFFFFFFF for v in out)
     assert bad == 0, f"{bad} differ, one of them {which:#010x}"

@@ -41,7 +41,8 @@ def test_gradients_of_many_wide_rows(rows, cols, dtype):
     assert torch.equal(over, dx)
     half, tiny = {torch.float32: (U, 2.0 ** -149), torch.bfloat16: (2.0 ** -8, 2.0 ** -133),
                   torch.float16: (2.0 ** -11, 2.0 ** -24)}[dtype]
-    want_g, size_g = torch.zeros(cols, dtype=torch.float64, device="cuda"), torch.zeros(cols, dtype=torch.float64, device="cuda")
+    want_g = torch.zeros(cols, dtype=torch.float64, device="cuda")
+    size_g = torch.zeros_like(want_g)
     for a in range(0, rows, 256):                     # the formula, 256 rows at a time
         at = slice(a, a + 256)
         r, d = rstd[at].double()[:, None], dy[at].double()
@@ -61,9 +62,9 @@ def test_gradients_of_many_wide_rows(rows, cols, dtype):
     assert torch.equal(alone, dx[part])
 
 
-@pytest.mark.parametrize("rows,cols,dtype,residual", [(8200, 8201, torch.bfloat16, True), (4100, 8200, torch.float32, True),
-                                                      (1100, 32768, torch.float32, False), (600, 32768, torch.bfloat16, True),
-                                                      (530000, 128, torch.float16, True)])
+@pytest.mark.parametrize("rows,cols,dtype,residual", [
+    (8200, 8201, torch.bfloat16, True), (4100, 8200, torch.float32, True), (1100, 32768, torch.float32, False),
+    (600, 32768, torch.bfloat16, True), (530000, 128, torch.float16, True)])
 def test_forward_past_the_caches(rows, cols, dtype, residual):
     """Inputs of more than 128 MiB (and one of 600 wide rows): scales and codes bit for bit, and the
     same bits as a few of the rows give alone."""

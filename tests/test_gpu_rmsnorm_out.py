@@ -42,7 +42,8 @@ def test_a_call_without_residual_lends_no_output(dtype, strided):
     plain = F.fp4root_rmsnorm_quantize(x, group=32, out=again)
     assert plain.h is x and torch.equal(again.h, want.h) and all(torch.equal(a, b) for a, b in zip(plain, first))
     # ... whose result lends no stream either, also where a field but h is replaced
-    for lent in (plain, plain._replace(y=torch.empty_like(plain.y)), F.fp4root_rmsnorm_quantize(x2, group=32, out=plain)):
+    for lent in (plain, plain._replace(y=torch.empty_like(plain.y)),
+                 F.fp4root_rmsnorm_quantize(x2, group=32, out=plain)):
         assert torch.equal(F.fp4root_rmsnorm_quantize(x2, None, r, group=32, out=lent).h, want.h)
         assert torch.equal(x, keep) and torch.equal(x2, keep2)
     assert all(torch.equal(a, b) for a, b in zip(F.fp4root_rmsnorm_quantize(x2, group=32, out=plain), alone))
